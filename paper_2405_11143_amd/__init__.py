@@ -15,4 +15,7 @@ from .pda import (EXPORTED, LIB_PATH, BoundCall, ModelStepGraph, PdaError, StepG
                   pda_problem, pda_status_string, pda_token_logprobs, pda_validate_host, pda_workspace_bytes,
                   pda_work_order, pda_decode_reusing_order, pda_decode_noalloc, bind_decode_noalloc,
                   bind_gather_ceiling, bind_stream_ceiling,
-                  pda_decode_append, bind_decode_append)
+                  pda_decode_append, bind_decode_append,
+                  pda_rotary, pda_rotary_scaling, pda_rotary_inv_freq, make_rotary, pda_rotary_apply, bind_rotary_apply,
+                  make_fp8_cache, pda_append_kv_fp8, bind_append_kv_fp8, pda_plan_fp8, pda_decode_fp8,
+                  bind_decode_fp8, pda_read_kv_fp8, bind_read_kv_fp8)

@@ -1,0 +1,223 @@
+// Pass 1 of attention over the 8-bit KV cache (include/pda_fp8.h); the order and
+// merge kernels are those of the bf16 cache.
+//
+// A work item is (partition of a context, sequence, KV head, tile of 16 query
+// rows): row r of a sequence and KV head is head r % G of its new token r / G.  The
+// 4 wavefronts of a workgroup take contiguous runs of the partition's blocks;
+// each streams them through registers and folds them with WaveAttention
+// (pda_wave.h), whose lanes want exactly what the layouts give: a 16-byte K
+// piece is the lane's A fragments of two k-steps, a V piece its 8 columns of
+// two of its four tokens.  Codes become bf16 in registers, two per instruction,
+// the row's power of two applied by the same instruction, so what is
+// folded is what a bf16 cache of the stored values would hold.
+#include "pda_fp8_internal.h"
+#include "pda_wave.h"
+
+namespace pda {
+namespace {
+
+constexpr int kThreads = kWaves * kWaveSize;
+
+template <int D>
+struct DecodeShared {
+  float o[kWaves][kFp8TileRows][D];
+  float m[kWaves][kFp8TileRows];
+  float l[kWaves][kFp8TileRows];
+  int bad[kWaves];
+};
+
+// One block's codes and scale bytes in a lane's registers.
+template <int D>
+struct Codes {
+  static constexpr int KP = D / 64;         // 16-byte K pieces of a lane
+  static constexpr int kTile = 16 * D;      // bytes of a K or V tile
+  uint4 k[KP], v[2];
+  unsigned ks, vs;  // the byte of the lane's K token; the bytes of its four V tokens
+
+  // Loads through descriptors of a tile's size: none leaves it, and with !needed
+  // (a length of zero) none touches memory.
+  __device__ __forceinline__ void load(const DecodeFp8Args& a, const char* kpool, const char* vpool,
+                                       const char* spool, size_t block, int phys, bool needed, int lane, bool& bad) {
+    if ((unsigned)phys >= (unsigned)a.step.num_blocks) {  // contract violation: never read outside the pool
+      bad = true;
+      phys = 0;
+    }
+    const size_t off = (size_t)phys * block;
+    const int bytes = needed ? kTile : 0;
+    const __amdgpu_buffer_rsrc_t rk = tile_rsrc(kpool + off * kTile, bytes);
+    const __amdgpu_buffer_rsrc_t rv = tile_rsrc(vpool + off * kTile, bytes);
+    const __amdgpu_buffer_rsrc_t rs = tile_rsrc(spool + off * 32, needed ? 32 : 0);
+    const int n = lane & 15, kg = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < KP; ++c) k[c] = load_stream(rk, 16 * lane + 1024 * c);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) v[j] = load_stream(rv, ((4 * j + kg) * (D / 8) + n % (D / 8)) * 16);
+    ks = __builtin_amdgcn_raw_buffer_load_b8(rs, n, 0, 0);
+    vs = __builtin_amdgcn_raw_buffer_load_b32(rs, 16 + 4 * kg, 0, 0);
+  }
+
+  __device__ __forceinline__ void convert(uint4 (&kr)[2 * KP], uint4 (&vr)[4]) const {
+    const float f = scale_of<0>(ks);
+#pragma unroll
+    for (int c = 0; c < KP; ++c) {
+      kr[2 * c] = to_bf16(k[c].x, k[c].y, f);
+      kr[2 * c + 1] = to_bf16(k[c].z, k[c].w, f);
+    }
+    vr[0] = to_bf16(v[0].x, v[0].y, scale_of<0>(vs));
+    vr[1] = to_bf16(v[0].z, v[0].w, scale_of<1>(vs));
+    vr[2] = to_bf16(v[1].x, v[1].y, scale_of<2>(vs));
+    vr[3] = to_bf16(v[1].z, v[1].w, scale_of<3>(vs));
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3)))
+decode_fp8_kernel(const DecodeFp8Args args) {
+  using WA = WaveAttention<D>;
+  using CD = Codes<D>;
+  __shared__ __align__(16) DecodeShared<D> sh;
+  const StepArgs& a = args.step;
+  const int tiles = a.num_chunk_groups;
+  int gt, b, p;  // KV head and tile, sequence, partition
+  if (a.order) {
+    const int item = a.order[blockIdx.x];
+    if ((unsigned)item >= (unsigned)a.num_regular_items) return;
+    const int HC = a.num_kv_heads * tiles;
+    gt = item % HC, b = item / HC % a.num_seqs, p = item / (HC * a.num_seqs);
+  } else {
+    gt = blockIdx.x, b = blockIdx.y, p = blockIdx.z;
+  }
+  const int g = gt / tiles, tile = gt % tiles;
+  const int G = a.group, n = a.num_query_tokens, Hq = a.num_q_heads, Tp = a.partition_tokens;
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWaveSize - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int L = clamped(a.lens[b], a.max_context_len);
+
+  const int r0 = tile * kFp8TileRows;
+  const int rows = min(kFp8TileRows, n * G - r0);
+  auto limit_of = [&](int r) { return L - n + 1 + r / G; };  // row r sees tokens below it
+  auto out_row = [&](int r) { return ((size_t)b * n + r / G) * Hq + (size_t)g * G + r % G; };
+  const int l_first = limit_of(r0);
+  const int l_vis = limit_of(r0 + rows - 1);
+  if (p == 0 && l_first <= 0) {  // rows that see nothing: zeros
+    for (int x = tid; x < rows * (D / 4); x += kThreads)
+      if (limit_of(r0 + x / (D / 4)) <= 0) store_nt4(a.out + out_row(r0 + x / (D / 4)) * D + 4 * (x % (D / 4)), 0.f, 0.f, 0.f, 0.f);
+  }
+  if (l_vis <= p * Tp) return;
+  const int j0 = p * Tp / kBlockTokens;
+  const int j1 = (min(l_vis, (p + 1) * Tp) + kBlockTokens - 1) / kBlockTokens;
+
+  WA wave(a.scale_log2);
+  {
+    const int r = r0 + min(lane & 15, rows - 1);  // lanes past the tile's last row repeat it
+    wave.start(a.q + out_row(r) * D, n - 1 - r / G);
+  }
+  const char* kpool = reinterpret_cast<const char*>(args.k) + (size_t)g * CD::kTile;
+  const char* vpool = reinterpret_cast<const char*>(args.v) + (size_t)g * CD::kTile;
+  const char* spool = reinterpret_cast<const char*>(args.scale) + (size_t)g * 32;
+  const int32_t* table_row = a.table + (size_t)b * a.max_blocks_per_seq;
+  const int per_slice = (j1 - j0 + kWaves - 1) / kWaves;
+  const int wj0 = min(j1, j0 + w * per_slice);
+  const int wj1 = min(j1, wj0 + per_slice);
+  bool bad = false;
+  CD c0, c1;
+  auto fold = [&](const CD& c, int j) {
+    uint4 kr[WA::NC], vr[4];
+    c.convert(kr, vr);
+    wave.process(kr, vr, j * kBlockTokens, L, l_first, l_vis);
+  };
+  for (int jc = wj0; jc < wj1; jc += kWaveSize) {
+    const int cn = min(kWaveSize, wj1 - jc);
+    const int ids = lane < cn ? table_row[jc + lane] : 0;
+    auto load = [&](CD& c, int i) {
+      c.load(args, kpool, vpool, spool, a.num_kv_heads, __builtin_amdgcn_readlane(ids, min(i, cn - 1)), i < cn, lane, bad);
+    };
+    load(c0, 0);
+    for (int i = 0; i < cn; i += 2) {
+      load(c1, i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      fold(c0, jc + i);
+      if (i + 1 >= cn) break;
+      load(c0, i + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      fold(c1, jc + i + 1);
+    }
+  }
+  wave.finish();
+
+  // ---- the wavefronts' states, merged in a fixed order ----
+  {
+    const int h = lane & 15;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d0 = wave.d_of(i, 0);
+      *reinterpret_cast<float4*>(&sh.o[w][h][d0]) = make_float4(wave.o[0][i], wave.o[1][i], wave.o[2][i], wave.o[3][i]);
+      if constexpr (D == 128)
+        *reinterpret_cast<float4*>(&sh.o[w][h][d0 + 4]) = make_float4(wave.o[4][i], wave.o[5][i], wave.o[6][i], wave.o[7][i]);
+    }
+    if (lane < 16) {
+      sh.m[w][h] = wave.m_run;
+      sh.l[w][h] = wave.l_run;
+    }
+    if (lane == 0) sh.bad[w] = bad ? 1 : 0;
+  }
+  __syncthreads();
+  int any_bad = 0;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) any_bad |= sh.bad[x];
+  for (int x = tid; x < rows * (D / 4); x += kThreads) {
+    const int h = x / (D / 4), d0 = 4 * (x % (D / 4));
+    const int limit = limit_of(r0 + h);
+    const int parts = limit > 0 ? (limit + Tp - 1) / Tp : 0;
+    if (p >= parts) continue;  // the row sees nothing here
+    float M = WA::kFloor, lsum = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) M = fmaxf(M, sh.m[y][h]);
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) {
+      const float s = exp2_fast(sh.m[y][h] - M);
+      const f32x4_t o = *reinterpret_cast<const f32x4_t*>(&sh.o[y][h][d0]);
+      lsum = fmaf(s, sh.l[y][h], lsum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(s, o[e], acc[e]);
+    }
+    if (any_bad) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_nanf("");
+    }
+    const size_t row = out_row(r0 + h);
+    if (parts == 1) {
+      const bool pos = lsum > 0.f;
+      store_nt4(a.out + row * D + d0, pos ? acc[0] / lsum : acc[0], pos ? acc[1] / lsum : acc[1],
+                pos ? acc[2] / lsum : acc[2], pos ? acc[3] / lsum : acc[3]);
+    } else {  // a partial state for the merge
+      const size_t slot = row * a.slots_per_row + p;
+      *reinterpret_cast<f32x4_t*>(a.part_o + slot * D + d0) = acc;
+      if (d0 == 0) {
+        a.part_m[slot] = M;
+        a.part_l[slot] = lsum;
+      }
+    }
+  }
+}
+
+template <int D>
+hipError_t launch_d(const DecodeFp8Args& a, hipStream_t stream) {
+  const StepArgs& s = a.step;
+  const dim3 grid = s.order ? dim3((unsigned)s.num_regular_items)
+                            : dim3((unsigned)s.num_kv_heads * (unsigned)s.num_chunk_groups, s.num_seqs, s.num_partitions);
+  hipLaunchKernelGGL(decode_fp8_kernel<D>, grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_decode_fp8(const DecodeFp8Args& a, int head_dim, hipStream_t stream) {
+  if (head_dim == 64) return launch_d<64>(a, stream);
+  if (head_dim == 128) return launch_d<128>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace pda

@@ -1,0 +1,69 @@
+// Rows of the 8-bit KV cache back as bf16 (include/pda_fp8.h): bound by memory,
+// 2 D + 2 bytes read and 4 D written per row and KV head.  A workgroup takes one
+// block of a sequence, a thread 8 elements of a row at a time (8 bytes read, 16
+// written), neighbouring threads neighbouring elements of the output.
+#include "pda_fp8_internal.h"
+
+namespace pda {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) read_fp8_kernel(const ReadFp8Args a, int blocks) {
+  constexpr int P = D / 8;  // pieces per row
+  for (int64_t bj = blockIdx.x; bj < (int64_t)a.num_seqs * blocks; bj += gridDim.x) {
+  const int b = (int)(bj / blocks);
+  const int j = (int)(bj % blocks);
+  const int L = clamped(a.lens[b], a.max_context_len);
+  const int first = a.first ? a.first[b] : 0;
+  const int64_t row0 = a.row_start[b];
+  // tokens [t_lo, t_hi) of this block go to rows row0 + t - first
+  const int64_t end = min((int64_t)L, first + (int64_t)a.row_start[b + 1] - row0);
+  const int t_lo = max(j * kBlockTokens, first);
+  const int t_hi = (int)min((int64_t)(j + 1) * kBlockTokens, end);
+  if (t_lo >= t_hi) continue;
+  const int page = a.table[(size_t)b * a.max_blocks_per_seq + j];
+  const bool ok = (unsigned)page < (unsigned)a.num_blocks;
+  const int H = a.num_kv_heads;
+  for (int x = threadIdx.x; x < (t_hi - t_lo) * H * P; x += kThreads) {
+    const int c = x % P;
+    const int g = x / P % H;
+    const int t = t_lo + x / P / H;
+    const int64_t row = row0 + ((int64_t)t - first);
+    if (row < 0 || row >= a.num_rows) continue;
+    const int o = t % kBlockTokens;
+    uint4 k = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u), v = k;  // NaN
+    if (ok) {
+      const size_t tile = (size_t)page * H + g;
+      const uint2 kc = *reinterpret_cast<const uint2*>(a.k + tile * (16 * D) + ((c / 8 * 4 + c % 4) * 16 + o) * 16 + c / 4 % 2 * 8);
+      const uint2 vc = *reinterpret_cast<const uint2*>(a.v + tile * (16 * D) + (((o / 2 % 2) * 4 + o / 4) * P + c) * 16 + o % 2 * 8);
+      const unsigned ks = a.scale[tile * 32 + o], vs = a.scale[tile * 32 + 16 + o];
+      // (the conversion takes a factor of 0 for 2^-127: a byte of 0 stands for zeros whatever the codes)
+      k = ks ? to_bf16(kc.x, kc.y, scale_of<0>(ks)) : make_uint4(0, 0, 0, 0);
+      v = vs ? to_bf16(vc.x, vc.y, scale_of<0>(vs)) : make_uint4(0, 0, 0, 0);
+    }
+    const size_t at = ((size_t)row * H + g) * P + c;
+    reinterpret_cast<uint4*>(a.k_out)[at] = k;
+    reinterpret_cast<uint4*>(a.v_out)[at] = v;
+  }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_read_fp8(const ReadFp8Args& a, int head_dim, hipStream_t stream) {
+  const int blocks = (a.max_context_len + kBlockTokens - 1) / kBlockTokens;
+  if (blocks == 0) return hipSuccess;
+  const dim3 grid((unsigned)min((int64_t)a.num_seqs * blocks, kMaxGrid));
+  if (head_dim == 64)
+    hipLaunchKernelGGL((read_fp8_kernel<64>), grid, dim3(kThreads), 0, stream, a, blocks);
+  else if (head_dim == 128)
+    hipLaunchKernelGGL((read_fp8_kernel<128>), grid, dim3(kThreads), 0, stream, a, blocks);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace pda

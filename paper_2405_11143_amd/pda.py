@@ -29,8 +29,10 @@ EXPORTED = ("pda_plan", "pda_workspace_bytes", "pda_decode", "pda_partition_atte
             "pda_validate_host", "pda_work_order", "pda_decode_reusing_order",
             "pda_partition_attention_reusing_order", "pda_decode_noalloc",
             "pda_gather_ceiling", "pda_stream_ceiling", "pda_model_step_graph_create", "pda_decode_append",
-            "pda_status_string")
+            "pda_rotary_inv_freq", "pda_rotary_apply", "pda_append_kv_fp8", "pda_plan_fp8", "pda_decode_fp8",
+            "pda_read_kv_fp8", "pda_status_string")
 PDA_DTYPE_BF16, PDA_DTYPE_F32 = 0, 1
+PDA_ROTARY_PLAIN, PDA_ROTARY_LINEAR, PDA_ROTARY_BASE, PDA_ROTARY_BANDS, PDA_ROTARY_RAMP = 0, 1, 2, 3, 4
 
 
 class pda_problem(ctypes.Structure):
@@ -56,6 +58,16 @@ class pda_prefix_groups(ctypes.Structure):
 class pda_layer_buffers(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
                 ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("out", ctypes.c_void_p)]
+
+
+class pda_rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("backward", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("inv_freq", ctypes.c_void_p)]
+
+
+class pda_rotary_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
 
 
 class PdaError(RuntimeError):
@@ -105,6 +117,14 @@ def load_library(path: str = LIB_PATH):
                                        ctypes.c_float, vp, vp, vp, sz, vp]
     lib.pda_logprob_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.pda_validate_host.argtypes = [P, vp, vp, ctypes.POINTER(ctypes.c_int64)]
+    c32, c64, dbl = ctypes.c_int32, ctypes.c_int64, ctypes.c_double
+    R = ctypes.POINTER(pda_rotary)
+    lib.pda_rotary_inv_freq.argtypes = [c32, dbl, ctypes.POINTER(pda_rotary_scaling), vp, ctypes.POINTER(ctypes.c_float)]
+    lib.pda_rotary_apply.argtypes = [R, c32, c32, c32, c32, c32, vp] + [vp, c64] * 4 + [vp]
+    lib.pda_append_kv_fp8.argtypes = [P, R] + [vp] * 9 + [vp]
+    lib.pda_plan_fp8.argtypes = [P, ctypes.POINTER(pda_plan_info)]
+    lib.pda_decode_fp8.argtypes = [P, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    lib.pda_read_kv_fp8.argtypes = [P] + [vp] * 7 + [c32, vp, vp, vp]
     lib.pda_status_string.argtypes = [i32]
     lib.pda_status_string.restype = ctypes.c_char_p
     for name in EXPORTED[:-1]:
@@ -658,3 +678,321 @@ def bind_stream_ceiling(buf, workgroups: int, sink=None, stream=None) -> BoundCa
     args = (buf.data_ptr(), ctypes.c_size_t(nbytes), int(workgroups), sink.data_ptr(),
             _stream_handle(stream, buf.device))
     return BoundCall("pda_stream_ceiling", args, (buf, sink), sink)
+
+
+# ---- the 8-bit KV cache and rotary positions (include/pda_fp8.h) ----
+
+class DeviceCall(BoundCall):
+    """A BoundCall that runs with its tensors' device current, whichever is
+    current where it is called."""
+
+    def __init__(self, fn_name, args, keep, device, result=None):
+        super().__init__(fn_name, args, keep, result)
+        import torch
+
+        self._index = device.index if device.index is not None else torch.cuda.current_device()
+        self._current, self._device = torch.cuda.current_device, torch.cuda.device
+
+    def __call__(self):
+        if self._current() != self._index:
+            with self._device(self._index):
+                return super().__call__()
+        return super().__call__()
+
+
+def _same_device(*tensors):
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on different devices: {sorted(map(str, devices))}")
+    return devices.pop()
+
+
+def _hold(stream, *temporaries):
+    """Tensors allocated for one call on a stream that is not the current one:
+    their memory is not reused before the stream is done with them."""
+    import torch
+
+    if stream is not None:
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream))
+        for t in temporaries:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _check_fp8_cache(k_cache, v_cache, kv_scale):
+    """(num_blocks, Hkv, D) of an 8-bit cache."""
+    import torch
+
+    for name, t, dt in (("k_cache", k_cache, torch.float8_e4m3fn), ("v_cache", v_cache, torch.float8_e4m3fn),
+                        ("kv_scale", kv_scale, torch.uint8)):
+        _require(name, t, dt)
+    if k_cache.dim() != 7 or tuple(k_cache.shape[3:]) != (4, 16, 2, 8):
+        raise ValueError("k_cache must be [num_blocks][Hkv][D/64][4][16][2][8]")
+    NB, Hkv, D = k_cache.shape[0], k_cache.shape[1], 64 * k_cache.shape[2]
+    if tuple(v_cache.shape) != (NB, Hkv, 2, 4, D // 8, 2, 8):
+        raise ValueError(f"v_cache must be [num_blocks][Hkv][2][4][D/8][2][8] = {(NB, Hkv, 2, 4, D // 8, 2, 8)}")
+    if tuple(kv_scale.shape) != (NB, Hkv, 2, 16):
+        raise ValueError(f"kv_scale must be [num_blocks][Hkv][2][16] = {(NB, Hkv, 2, 16)}")
+    return NB, Hkv, D
+
+
+def _check_paged(block_table, context_lens, B):
+    import torch
+
+    _require("block_table", block_table, torch.int32)
+    _require("context_lens", context_lens, torch.int32)
+    if block_table.dim() != 2 or block_table.shape[0] != B or context_lens.shape != (B,):
+        raise ValueError("block_table [B][max_blocks], context_lens [B]")
+
+
+def make_fp8_cache(num_blocks: int, num_kv_heads: int, head_dim: int, device="cuda"):
+    """An empty 8-bit cache: (k_cache, v_cache, kv_scale), all zero."""
+    import torch
+
+    z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+    return (z(num_blocks, num_kv_heads, head_dim // 64, 4, 16, 2, 8).view(torch.float8_e4m3fn),
+            z(num_blocks, num_kv_heads, 2, 4, head_dim // 8, 2, 8).view(torch.float8_e4m3fn),
+            z(num_blocks, num_kv_heads, 2, 16))
+
+
+def pda_rotary_inv_freq(rotary_dim: int, base: float = 10000.0, kind: int = PDA_ROTARY_PLAIN, factor: float = 1.0,
+                        original_len: float = 0.0, low: float = 0.0, high: float = 0.0):
+    """(inv_freq, magnitude): the rotary_dim / 2 frequencies base^(-2i / rotary_dim)
+    scaled for long contexts as `kind` says (include/pda_fp8.h), as a float64
+    numpy array, and the factor on the rotated elements."""
+    inv_freq = np.empty(max(int(rotary_dim), 0) // 2, dtype=np.float64)
+    scaling = pda_rotary_scaling(int(kind), float(factor), float(original_len), float(low), float(high))
+    magnitude = ctypes.c_float()
+    rc = load_library().pda_rotary_inv_freq(int(rotary_dim), float(base), ctypes.byref(scaling), inv_freq.ctypes.data,
+                                            ctypes.byref(magnitude))
+    if rc != PDA_OK:
+        raise PdaError(rc, "pda_rotary_inv_freq")
+    return inv_freq, magnitude.value
+
+
+def make_rotary(inv_freq, interleaved: bool = False, backward: bool = False, magnitude: float = 1.0) -> pda_rotary:
+    """A rotary embedding of the first 2 * len(inv_freq) elements of every head
+    row; inv_freq: float64 device tensor (it is kept alive by the result)."""
+    import torch
+
+    _require("inv_freq", inv_freq, torch.float64)
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must be [rotary_dim / 2]")
+    r = pda_rotary(2 * inv_freq.shape[0], int(bool(interleaved)), int(bool(backward)), float(magnitude),
+                   inv_freq.data_ptr())
+    r.tensor = inv_freq
+    return r
+
+
+def _token_rows(name, t, dtype):
+    """Token stride of rows [T][H][D] whose heads are contiguous."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    T, H, D = t.shape
+    if t.numel() and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+        raise ValueError(f"{name} must be [T][H][D] with the heads of a token contiguous")
+    return t.stride(0) if T > 1 else H * D  # (the stride of a single token is free)
+
+
+def bind_rotary_apply(q, positions, rotary: pda_rotary, k=None, q_out=None, k_out=None, stream=None) -> DeviceCall:
+    """pda_rotary_apply bound to these tensors and the given (else the current)
+    stream; calling it returns (q_out, k_out).  q [T][Hq][D] and k [T][Hkv][D]
+    are bf16 or float32 with any token stride; the outputs are allocated when
+    not given, and may be the inputs (in place).  positions int32 [T], negative:
+    padding, left alone."""
+    import torch
+
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("q must be bfloat16 or float32")
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise ValueError("q [T][Hq][D], k [T][Hkv][D]")
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    _require("positions", positions, torch.int32)
+    if positions.shape != (q.shape[0],):
+        raise ValueError("positions must be [T]")
+    # (padding rows are not written: an output made here holds zeros there)
+    q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = torch.zeros(k.shape, dtype=k.dtype, device=k.device)
+    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
+        raise ValueError("the outputs must have the inputs' shapes")
+    device = _same_device(q, q_out, k, k_out, positions, rotary.tensor)
+    T, Hq, D = q.shape
+    rows = [q.data_ptr(), _token_rows("q", q, q.dtype), q_out.data_ptr(), _token_rows("q_out", q_out, q.dtype)]
+    if k is not None:
+        rows += [k.data_ptr(), _token_rows("k", k, q.dtype), k_out.data_ptr(), _token_rows("k_out", k_out, q.dtype)]
+    else:
+        rows += [None, 0, None, 0]
+    dtype = PDA_DTYPE_BF16 if q.dtype == torch.bfloat16 else PDA_DTYPE_F32
+    args = (ctypes.byref(rotary), T, Hq, 0 if k is None else k.shape[1], D, dtype, positions.data_ptr(), *rows,
+            _stream_handle(stream, device))
+    return DeviceCall("pda_rotary_apply", args, (rotary, q, q_out, k, k_out, positions), device, (q_out, k_out))
+
+
+def pda_rotary_apply(q, positions, rotary: pda_rotary, k=None, q_out=None, k_out=None, stream=None):
+    """Rotary positions of q (and k) rows; returns (q_out, k_out or None).  See
+    bind_rotary_apply."""
+    call = bind_rotary_apply(q, positions, rotary, k, q_out, k_out, stream)
+    result = call()
+    _hold(stream, *result)
+    return result
+
+
+def bind_append_kv_fp8(k_new, v_new, block_table, context_lens, k_cache, v_cache, kv_scale, *, max_context_len: int,
+                       rotary: pda_rotary = None, q=None, q_out=None, num_q_heads: int = None,
+                       stream=None) -> DeviceCall:
+    """pda_append_kv_fp8 bound to these tensors and the given (else the current)
+    stream: k_new/v_new bf16 [B][n][Hkv][D] quantised and stored at positions
+    L - n .. L - 1 of the 8-bit cache (make_fp8_cache); with `rotary` the keys are
+    rotated first, and q (bf16 [B][n][Hq][D] or, for n = 1, [B][Hq][D]) into q_out
+    (allocated when not given; may be q).  Calling it returns q_out (None without
+    q)."""
+    import torch
+
+    NB, Hkv, D = _check_fp8_cache(k_cache, v_cache, kv_scale)
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be [B][n][Hkv][D]")
+    B, n = k_new.shape[:2]
+    _check_paged(block_table, context_lens, B)
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        _require(name, t, torch.bfloat16)
+        if tuple(t.shape) != (B, n, Hkv, D):
+            raise ValueError(f"k_new and v_new must be [B][n][Hkv][D] = {(B, n, Hkv, D)}")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    Hq = Hkv if num_q_heads is None else num_q_heads
+    if q is not None:
+        if rotary is None:
+            raise ValueError("q is rotated here: give `rotary`")
+        _require("q", q, torch.bfloat16)
+        if _query_shape(q)[:2] != (B, n) or q.shape[-1] != D:
+            raise ValueError("q must be [B][n][Hq][D]")
+        Hq = q.shape[-2]
+        if q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        _require("q_out", q_out, torch.bfloat16)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    device = _same_device(k_new, v_new, block_table, context_lens, k_cache, v_cache, kv_scale, q, q_out,
+                          rotary.tensor if rotary is not None else None)
+    if n == 0:
+        raise ValueError("at least one new token")
+    prob = make_problem(B, Hq, Hkv, D, NB, block_table.shape[1], max_context_len, 0, 16, n)
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    args = (ctypes.byref(prob), ctypes.byref(rotary) if rotary is not None else None, ptr(q), ptr(q_out),
+            k_new.data_ptr(), v_new.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(), k_cache.data_ptr(),
+            v_cache.data_ptr(), kv_scale.data_ptr(), _stream_handle(stream, device))
+    keep = (prob, rotary, q, q_out, k_new, v_new, block_table, context_lens, k_cache, v_cache, kv_scale)
+    return DeviceCall("pda_append_kv_fp8", args, keep, device, q_out)
+
+
+def pda_append_kv_fp8(k_new, v_new, block_table, context_lens, k_cache, v_cache, kv_scale, *, max_context_len: int,
+                      rotary: pda_rotary = None, q=None, q_out=None, num_q_heads: int = None, stream=None):
+    """The new tokens' K/V rows (rotated, when `rotary` is given) quantised and
+    stored in the 8-bit cache, in place; returns the rotated queries (None without
+    q).  See bind_append_kv_fp8."""
+    result = bind_append_kv_fp8(k_new, v_new, block_table, context_lens, k_cache, v_cache, kv_scale,
+                                max_context_len=max_context_len, rotary=rotary, q=q, q_out=q_out,
+                                num_q_heads=num_q_heads, stream=stream)()
+    _hold(stream, result)
+    return result
+
+
+def pda_plan_fp8(prob: pda_problem) -> dict:
+    """The plan of pda_decode_fp8: partition_tokens, num_partitions, workspace_bytes."""
+    info = pda_plan_info()
+    rc = load_library().pda_plan_fp8(ctypes.byref(prob), ctypes.byref(info))
+    if rc != PDA_OK:
+        raise PdaError(rc, "pda_plan_fp8")
+    return info.as_dict()
+
+
+def bind_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, scale: float, out=None, *,
+                    max_context_len: int, partition_tokens: int = 0, workspace=None, stream=None) -> DeviceCall:
+    """pda_decode_fp8 bound to these tensors and the given (else the current)
+    stream: the attention of bind_decode over an 8-bit cache (make_fp8_cache).
+    `workspace` (uint8, pda_plan_fp8's workspace_bytes) is allocated here when not
+    given."""
+    import torch
+
+    NB, Hkv, D = _check_fp8_cache(k_cache, v_cache, kv_scale)
+    _require("q", q, torch.bfloat16)
+    B, n, Hq, Dq = _query_shape(q)
+    if Dq != D:
+        raise ValueError("q and the caches disagree on the head size")
+    if n == 0:
+        raise ValueError("at least one new token")
+    _check_paged(block_table, context_lens, B)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+    _require("out", out, torch.float32)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    device = _same_device(q, k_cache, v_cache, kv_scale, block_table, context_lens, out, workspace)
+    prob = make_problem(B, Hq, Hkv, D, NB, block_table.shape[1], max_context_len, partition_tokens, 16, n)
+    need = pda_plan_fp8(prob)["workspace_bytes"]
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    ws_ptr = workspace.data_ptr() if workspace is not None else None
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    args = (ctypes.byref(prob), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv_scale.data_ptr(),
+            block_table.data_ptr(), context_lens.data_ptr(), ctypes.c_float(scale), out.data_ptr(), ws_ptr, ws_bytes,
+            _stream_handle(stream, device))
+    keep = (prob, q, k_cache, v_cache, kv_scale, block_table, context_lens, out, workspace)
+    call = DeviceCall("pda_decode_fp8", args, keep, device, out)
+    call.workspace = workspace
+    return call
+
+
+def pda_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, scale: float, out=None, *,
+                   max_context_len: int, partition_tokens: int = 0, workspace=None, stream=None):
+    """One attention step over an 8-bit cache; the other arguments are those of
+    pda_decode.  Returns out (fp32, shaped like q)."""
+    call = bind_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, scale, out,
+                           max_context_len=max_context_len, partition_tokens=partition_tokens, workspace=workspace,
+                           stream=stream)
+    result = call()
+    _hold(stream, result, call.workspace)
+    return result
+
+
+def bind_read_kv_fp8(k_cache, v_cache, kv_scale, block_table, context_lens, row_start, k_out, v_out, *,
+                     max_context_len: int, first_token=None, stream=None) -> DeviceCall:
+    """pda_read_kv_fp8 bound to these tensors and the given (else the current)
+    stream: tokens first_token[b], ... (from 0 without it) of every sequence into
+    rows row_start[b] .. row_start[b + 1] - 1 of k_out and v_out (bf16
+    [rows][Hkv][D]).  Calling it returns (k_out, v_out)."""
+    import torch
+
+    NB, Hkv, D = _check_fp8_cache(k_cache, v_cache, kv_scale)
+    B = block_table.shape[0]
+    _check_paged(block_table, context_lens, B)
+    _require("row_start", row_start, torch.int32)
+    if row_start.shape != (B + 1,):
+        raise ValueError("row_start must be [B + 1]")
+    if first_token is not None:
+        _require("first_token", first_token, torch.int32)
+        if first_token.shape != (B,):
+            raise ValueError("first_token must be [B]")
+    _require("k_out", k_out, torch.bfloat16)
+    _require("v_out", v_out, torch.bfloat16)
+    if k_out.dim() != 3 or tuple(k_out.shape[1:]) != (Hkv, D) or v_out.shape != k_out.shape:
+        raise ValueError("k_out and v_out must be [rows][Hkv][D]")
+    device = _same_device(k_cache, v_cache, kv_scale, block_table, context_lens, row_start, first_token, k_out, v_out)
+    prob = make_problem(B, Hkv, Hkv, D, NB, block_table.shape[1], max_context_len)
+    args = (ctypes.byref(prob), k_cache.data_ptr(), v_cache.data_ptr(), kv_scale.data_ptr(), block_table.data_ptr(),
+            context_lens.data_ptr(), first_token.data_ptr() if first_token is not None else None, row_start.data_ptr(),
+            k_out.shape[0], k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream, device))
+    keep = (prob, k_cache, v_cache, kv_scale, block_table, context_lens, first_token, row_start, k_out, v_out)
+    return DeviceCall("pda_read_kv_fp8", args, keep, device, (k_out, v_out))
+
+
+def pda_read_kv_fp8(k_cache, v_cache, kv_scale, block_table, context_lens, row_start, k_out, v_out, *,
+                    max_context_len: int, first_token=None, stream=None):
+    """Rows of the 8-bit cache back as contiguous bf16.  See bind_read_kv_fp8."""
+    return bind_read_kv_fp8(k_cache, v_cache, kv_scale, block_table, context_lens, row_start, k_out, v_out,
+                            max_context_len=max_context_len, first_token=first_token, stream=stream)()

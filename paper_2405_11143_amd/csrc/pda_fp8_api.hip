@@ -51,7 +51,8 @@ int make_plan(const pda_problem* p, Plan* plan) {
   if (rc != PDA_OK) return rc;
   const int n = query_tokens(p);
   const int64_t rows = (int64_t)n * (p->num_q_heads / p->num_kv_heads);
-  plan->tiles = (int)((rows + pda::kFp8TileRows - 1) / pda::kFp8TileRows);
+  const int item_rows = rows <= pda::kFp8TileRows ? pda::kFp8TileRows : 2 * pda::kFp8TileRows;
+  plan->tiles = (int)((rows + item_rows - 1) / item_rows);
   const int64_t parts = plan->info.num_partitions;
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
   const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads * plan->tiles;

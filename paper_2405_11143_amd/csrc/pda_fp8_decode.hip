@@ -18,11 +18,11 @@ namespace {
 
 constexpr int kThreads = kWaves * kWaveSize;
 
-template <int D>
+template <int D, int ROWS>
 struct DecodeShared {
-  float o[kWaves][kFp8TileRows][D];
-  float m[kWaves][kFp8TileRows];
-  float l[kWaves][kFp8TileRows];
+  float o[kWaves][ROWS][D];
+  float m[kWaves][ROWS];
+  float l[kWaves][ROWS];
   int bad[kWaves];
 };
 
@@ -70,12 +70,83 @@ struct Codes {
   }
 };
 
+// The fold of one block, on converted tiles, into the states of NT tiles of 16
+// rows.  As WaveAttention::process, but each probability is split into three bf16
+// parts, each the top 16 bits of what is left, which together are all of its 24
+// bits: the third costs MFMAs that the wait for memory hides (with two the result
+// was 4.8e-6 of its norm off, ten times what the rest of the arithmetic is).
 template <int D>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3)))
+struct Fold : WaveAttention<D> {
+  using WA = WaveAttention<D>;
+  __device__ __forceinline__ Fold() : WA(0.f) {}
+  struct Parts {
+    shortx4_t p[3];
+  };
+
+  __device__ __forceinline__ Parts parts(const uint4 (&kr)[1][WA::NC], int tok0, int L, bool tail) {
+    float sc[1][4];
+    this->template scores<1>(kr, sc);
+    if (tail) {
+      asm volatile("");  // a branch: as selects the masking would run on every block
+      const int rel = L - this->lim_off - (tok0 + 4 * this->kg);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= rel) sc[0][i] = WA::kNegInf;
+    }
+    const float top = max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], WA::kNegInf);
+    if (__builtin_amdgcn_ballot_w64(top > this->m_run + WA::kRescaleSlack) != 0) this->rescale(top);
+    float pr[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pr[i] = exp2_fast(sc[0][i] - this->m_run);
+    this->l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+    Parts f;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      unsigned w[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) w[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
+      f.p[k] = __builtin_bit_cast(shortx4_t, make_uint2(w[0], w[1]));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pr[i] -= __uint_as_float(__float_as_uint(pr[i]) & 0xffff0000u);
+    }
+    return f;
+  }
+
+  // The A fragment of output tile t: 4 tokens of one column.
+  __device__ __forceinline__ shortx4_t v_frag(const uint4 (&vr)[4], int t) const {
+    const bool hi = t & 1;
+    return __builtin_bit_cast(shortx4_t,
+                              make_uint2(pack_halves(this->col_dword(vr, 0, t), this->col_dword(vr, 1, t), hi),
+                                         pack_halves(this->col_dword(vr, 2, t), this->col_dword(vr, 3, t), hi)));
+  }
+};
+
+template <int D, int NT>
+__device__ __forceinline__ void fold_block(Fold<D> (&wave)[NT], const uint4 (&kr)[1][WaveAttention<D>::NC], uint4 (&vr)[4],
+                                           int tok0, int L, int l_first, int l_vis) {
+  const bool tail = tok0 + kBlockTokens > l_first;  // wavefront-uniform
+  typename Fold<D>::Parts f[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) f[x] = wave[x].parts(kr, tok0, L, tail);
+  wave[0].mask_v(vr, tok0, l_vis, tail);
+#pragma unroll
+  for (int t = 0; t < WaveAttention<D>::VT; ++t) {
+    const shortx4_t a = wave[0].v_frag(vr, t);
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) wave[x].o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, f[x].p[k], wave[x].o[t], 0, 0, 0);
+  }
+}
+
+// NT: tiles of 16 query rows of a work item (1 or 2), folded from the same
+// converted blocks.
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2)))
 decode_fp8_kernel(const DecodeFp8Args args) {
   using WA = WaveAttention<D>;
   using CD = Codes<D>;
-  __shared__ __align__(16) DecodeShared<D> sh;
+  __shared__ __align__(16) DecodeShared<D, NT * kFp8TileRows> sh;
   const StepArgs& a = args.step;
   const int tiles = a.num_chunk_groups;
   int gt, b, p;  // KV head and tile, sequence, partition
@@ -94,8 +165,8 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int L = clamped(a.lens[b], a.max_context_len);
 
-  const int r0 = tile * kFp8TileRows;
-  const int rows = min(kFp8TileRows, n * G - r0);
+  const int r0 = tile * (NT * kFp8TileRows);
+  const int rows = min(NT * kFp8TileRows, n * G - r0);
   auto limit_of = [&](int r) { return L - n + 1 + r / G; };  // row r sees tokens below it
   auto out_row = [&](int r) { return ((size_t)b * n + r / G) * Hq + (size_t)g * G + r % G; };
   const int l_first = limit_of(r0);
@@ -108,10 +179,12 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   const int j0 = p * Tp / kBlockTokens;
   const int j1 = (min(l_vis, (p + 1) * Tp) + kBlockTokens - 1) / kBlockTokens;
 
-  WA wave(a.scale_log2);
-  {
-    const int r = r0 + min(lane & 15, rows - 1);  // lanes past the tile's last row repeat it
-    wave.start(a.q + out_row(r) * D, n - 1 - r / G);
+  Fold<D> wave[NT];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    wave[x].scale_log2 = a.scale_log2;
+    const int r = r0 + min(x * kFp8TileRows + (lane & 15), rows - 1);  // lanes past the last row repeat it
+    wave[x].start(a.q + out_row(r) * D, n - 1 - r / G);
   }
   const char* kpool = reinterpret_cast<const char*>(args.k) + (size_t)g * CD::kTile;
   const char* vpool = reinterpret_cast<const char*>(args.v) + (size_t)g * CD::kTile;
@@ -123,9 +196,9 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   bool bad = false;
   CD c0, c1;
   auto fold = [&](const CD& c, int j) {
-    uint4 kr[WA::NC], vr[4];
-    c.convert(kr, vr);
-    wave.process(kr, vr, j * kBlockTokens, L, l_first, l_vis);
+    uint4 kr[1][WA::NC], vr[4];
+    c.convert(kr[0], vr);
+    fold_block<D, NT>(wave, kr, vr, j * kBlockTokens, L, l_first, l_vis);
   };
   for (int jc = wj0; jc < wj1; jc += kWaveSize) {
     const int cn = min(kWaveSize, wj1 - jc);
@@ -144,24 +217,25 @@ decode_fp8_kernel(const DecodeFp8Args args) {
       fold(c1, jc + i + 1);
     }
   }
-  wave.finish();
 
   // ---- the wavefronts' states, merged in a fixed order ----
-  {
-    const int h = lane & 15;
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    wave[x].finish();
+    const int h = x * kFp8TileRows + (lane & 15);
+    const f32x4_t* o = reinterpret_cast<const f32x4_t*>(wave[x].o);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int d0 = wave.d_of(i, 0);
-      *reinterpret_cast<float4*>(&sh.o[w][h][d0]) = make_float4(wave.o[0][i], wave.o[1][i], wave.o[2][i], wave.o[3][i]);
-      if constexpr (D == 128)
-        *reinterpret_cast<float4*>(&sh.o[w][h][d0 + 4]) = make_float4(wave.o[4][i], wave.o[5][i], wave.o[6][i], wave.o[7][i]);
+      const int d0 = wave[x].d_of(i, 0);
+      *reinterpret_cast<float4*>(&sh.o[w][h][d0]) = make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
+      if constexpr (D == 128) *reinterpret_cast<float4*>(&sh.o[w][h][d0 + 4]) = make_float4(o[4][i], o[5][i], o[6][i], o[7][i]);
     }
     if (lane < 16) {
-      sh.m[w][h] = wave.m_run;
-      sh.l[w][h] = wave.l_run;
+      sh.m[w][h] = wave[x].m_run;
+      sh.l[w][h] = wave[x].l_run;
     }
-    if (lane == 0) sh.bad[w] = bad ? 1 : 0;
   }
+  if (lane == 0) sh.bad[w] = bad ? 1 : 0;
   __syncthreads();
   int any_bad = 0;
 #pragma unroll
@@ -208,7 +282,10 @@ hipError_t launch_d(const DecodeFp8Args& a, hipStream_t stream) {
   const StepArgs& s = a.step;
   const dim3 grid = s.order ? dim3((unsigned)s.num_regular_items)
                             : dim3((unsigned)s.num_kv_heads * (unsigned)s.num_chunk_groups, s.num_seqs, s.num_partitions);
-  hipLaunchKernelGGL(decode_fp8_kernel<D>, grid, dim3(kThreads), 0, stream, a);
+  if (s.num_query_tokens * s.group <= kFp8TileRows)
+    hipLaunchKernelGGL((decode_fp8_kernel<D, 1>), grid, dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((decode_fp8_kernel<D, 2>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

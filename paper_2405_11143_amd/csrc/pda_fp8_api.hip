@@ -51,7 +51,7 @@ int make_plan(const pda_problem* p, Plan* plan) {
   if (rc != PDA_OK) return rc;
   const int n = query_tokens(p);
   const int64_t rows = (int64_t)n * (p->num_q_heads / p->num_kv_heads);
-  const int item_rows = rows <= pda::kFp8TileRows ? pda::kFp8TileRows : 2 * pda::kFp8TileRows;
+  const int item_rows = pda::fp8_item_rows(rows);
   plan->tiles = (int)((rows + item_rows - 1) / item_rows);
   const int64_t parts = plan->info.num_partitions;
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
@@ -223,6 +223,7 @@ int pda_decode_fp8(const pda_problem* prob, const void* q, const void* k_cache, 
   s.num_q_heads = prob->num_q_heads;
   s.num_kv_heads = prob->num_kv_heads;
   s.group = prob->num_q_heads / prob->num_kv_heads;
+  s.group_inverse = (65536 + s.group - 1) / s.group;
   s.num_blocks = prob->num_blocks;
   s.max_blocks_per_seq = prob->max_blocks_per_seq;
   s.max_context_len = prob->max_context_len;

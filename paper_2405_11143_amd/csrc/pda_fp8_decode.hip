@@ -280,6 +280,7 @@ decode_fp8_kernel(const DecodeFp8Args args) {
 template <int D>
 hipError_t launch_d(const DecodeFp8Args& a, hipStream_t stream) {
   const StepArgs& s = a.step;
+  if (s.num_query_tokens * s.group > 2 * kFp8TileRows) return launch_wide_fp8(a, D, stream);
   const dim3 grid = s.order ? dim3((unsigned)s.num_regular_items)
                             : dim3((unsigned)s.num_kv_heads * (unsigned)s.num_chunk_groups, s.num_seqs, s.num_partitions);
   if (s.num_query_tokens * s.group <= kFp8TileRows)

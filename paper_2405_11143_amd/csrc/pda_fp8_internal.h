@@ -74,10 +74,14 @@ struct ReadFp8Args {
 hipError_t launch_rotary(const RotaryApplyArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_append_fp8(const AppendFp8Args& a, int head_dim, hipStream_t stream);
 hipError_t launch_decode_fp8(const DecodeFp8Args& a, int head_dim, hipStream_t stream);
+hipError_t launch_wide_fp8(const DecodeFp8Args& a, int head_dim, hipStream_t stream);  // more than 32 rows
 hipError_t launch_read_fp8(const ReadFp8Args& a, int head_dim, hipStream_t stream);
 
-// Query rows of a work item's tile: one MFMA tile of 16.
-constexpr int kFp8TileRows = 16;
+constexpr int kFp8TileRows = 16;  // query rows of an MFMA tile of the decode kernel
+
+// Query rows of a work item whose sequence and KV head has `rows` of them: one or
+// two tiles of the decode kernel, or the rows of a workgroup of the wide one.
+inline int fp8_item_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 // ---- device helpers ----
 

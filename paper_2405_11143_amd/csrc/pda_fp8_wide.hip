@@ -20,6 +20,8 @@
 //    one after is being written; its successor's codes are in flight.
 //  * Rows are dense (no chunks of whole tokens): 7 heads per KV head fill the
 //    tiles as well as 8.
+#include <type_traits>
+
 #include "pda_fp8_internal.h"
 #include "pda_wave.h"
 
@@ -163,33 +165,35 @@ wide_fp8_kernel(const DecodeFp8Args args) {
   auto side_of = [&](int k) {
     return kOneSide ? k / (NP / 2 + (NP < 2)) : __builtin_amdgcn_readfirstlane((k * kThreads + w * kWaveSize) / (kStageBlocks * D));
   };
+  int ids = 0;  // lane x: the id of block 64 (block / 64) + x of the window
   auto issue = [&](int step) {
+    const int j = step * kStageBlocks;
+    if (j % kWaveSize == 0) ids = st.ids[j + lane];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
       const int blk = __builtin_amdgcn_readfirstlane((k * kThreads + w * kWaveSize) / D % kStageBlocks);
-      const int id = __builtin_amdgcn_readfirstlane(st.ids[step * kStageBlocks + blk]);
-      const size_t tile = (size_t)(unsigned)id * a.num_kv_heads + g;
+      const size_t tile = (size_t)(unsigned)__builtin_amdgcn_readlane(ids, j % kWaveSize + blk) * a.num_kv_heads + g;
       const uint8_t* pool = side_of(k) == 0 ? args.k : args.v;
       const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(tile_rsrc(pool + tile * kTile, kTile), g_off[k], 0, 0);
       raw[k] = make_uint4(t[0], t[1], t[2], t[3]);
-      const __amdgpu_buffer_rsrc_t rs = tile_rsrc(args.scale + tile * 32, 32);
-      raw_scale[k] = side_of(k) == 0 ? (unsigned)__builtin_amdgcn_raw_buffer_load_b8(rs, s_off[k], 0, 0) * 0x101u
-                                     : (unsigned)__builtin_amdgcn_raw_buffer_load_b16(rs, s_off[k], 0, 0);
+      // (two bytes, of which a K piece uses the first: past the last slot it reads V's first byte)
+      raw_scale[k] = __builtin_amdgcn_raw_buffer_load_b16(tile_rsrc(args.scale + tile * 32, 32), s_off[k], 0, 0);
     }
   };
-  auto commit = [&](int step, int tok0) {
-    uint4* buf = &st.buf[step % kBuffers][0][0];
+  auto commit = [&](uint4* buf, int tok0) {
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      uint4 lo = to_bf16(raw[k].x, raw[k].y, scale_of<0>(raw_scale[k]));
-      uint4 hi = to_bf16(raw[k].z, raw[k].w, scale_of<1>(raw_scale[k]));
-      if (tok0 + kStageBlocks * kBlockTokens > L) {  // uniform: values past the context are zeros whatever the slots hold
+      const bool is_k = side_of(k) == 0;
+      const float f0 = scale_of<0>(raw_scale[k]);
+      const float f1 = is_k ? f0 : scale_of<1>(raw_scale[k]);
+      uint4 lo = to_bf16(raw[k].x, raw[k].y, f0);
+      uint4 hi = to_bf16(raw[k].z, raw[k].w, f1);
+      if (!is_k && tok0 + kStageBlocks * kBlockTokens > L) {  // values past the context are zeros whatever the slots hold
+        asm volatile("");  // a branch
         const int blk = (k * kThreads + tid) / D % kStageBlocks;
         const int t = tok0 + blk * kBlockTokens + s_off[k] - 16;
-        if (side_of(k) == 1) {
-          if (t >= L) lo = make_uint4(0u, 0u, 0u, 0u);
-          if (t + 1 >= L) hi = make_uint4(0u, 0u, 0u, 0u);
-        }
+        if (t >= L) lo = make_uint4(0u, 0u, 0u, 0u);
+        if (t + 1 >= L) hi = make_uint4(0u, 0u, 0u, 0u);
       }
       buf[dst[k][0]] = lo;
       buf[dst[k][1]] = hi;
@@ -299,7 +303,8 @@ wide_fp8_kernel(const DecodeFp8Args args) {
   for (int jw = J0; jw < J1; jw += kWindow) {
     const int jwe = min(J1, jw + kWindow);
     const int nsteps = (jwe - jw + kStageBlocks - 1) / kStageBlocks;
-    for (int x = tid; x < nsteps * kStageBlocks; x += kThreads) {
+    const int n_ids = (nsteps * kStageBlocks + kWaveSize - 1) / kWaveSize * kWaveSize;  // (they are read 64 at a time)
+    for (int x = tid; x < n_ids; x += kThreads) {
       const int id = table_row[min(jw + x, jwe - 1)];  // past the end: the last block again (masked)
       const bool ok = (unsigned)id < (unsigned)a.num_blocks;  // never read outside the pool
       bad |= !ok;
@@ -311,7 +316,7 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     for (int x = 0; x < kBuffers - 1; ++x)
       if (x < nsteps) {
         issue(x);
-        commit(x, tok_w + 32 * x);
+        commit(st.buf[x][0], tok_w + 32 * x);
       }
     if (kBuffers - 1 < nsteps) issue(kBuffers - 1);
     __syncthreads();
@@ -320,14 +325,21 @@ wide_fp8_kernel(const DecodeFp8Args args) {
       largest();
       mask(tok_w);
     }
-    for (int step = 0; step < nsteps; ++step) {
+    // Step `step` is in buffer B = step % kBuffers (a constant, and so are all LDS
+    // addresses: the loop is unrolled by the buffers).  False at the last step.
+    auto one = [&](auto B, int step) {
       const int tok0 = tok_w + 32 * step;
       // behind the barrier the last step's buffer is free, and the next step's written
       if (step > 0) __syncthreads();
-      if (step + 2 < nsteps) commit(step + 2, tok0 + 64);
+      if (step + 2 < nsteps) commit(st.buf[(B + 2) % kBuffers][0], tok0 + 64);
       if (step + 3 < nsteps) issue(step + 3);
-      if (active && tok0 < l_vis)  // wavefront-uniform
-        fold(tok0, st.buf[step % kBuffers][0], st.buf[(step + 1) % kBuffers][0]);
+      if (active && tok0 < l_vis) fold(tok0, st.buf[B][0], st.buf[(B + 1) % kBuffers][0]);  // wavefront-uniform
+      return step + 1 < nsteps;
+    };
+    for (int step = 0;; step += kBuffers) {
+      if (!one(std::integral_constant<int, 0>{}, step)) break;
+      if (!one(std::integral_constant<int, 1>{}, step + 1)) break;
+      if (!one(std::integral_constant<int, 2>{}, step + 2)) break;
     }
     __syncthreads();
   }

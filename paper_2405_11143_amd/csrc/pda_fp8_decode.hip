@@ -31,8 +31,8 @@ template <int D>
 struct Codes {
   static constexpr int KP = D / 64;         // 16-byte K pieces of a lane
   static constexpr int kTile = 16 * D;      // bytes of a K or V tile
-  uint4 k[KP], v[2];
-  unsigned ks, vs;  // the byte of the lane's K token; the bytes of its four V tokens
+  uint4 k[KP], v[2];  // v: rows 4kg (x, y: 8 columns) and 4kg + 1 (z, w), then 4kg + 2 and 4kg + 3
+  unsigned ks, vs;    // the byte of the lane's K token; the bytes of its four V tokens
 
   // Loads through descriptors of a tile's size: none leaves it, and with !needed
   // (a length of zero) none touches memory.
@@ -56,86 +56,118 @@ struct Codes {
     vs = __builtin_amdgcn_raw_buffer_load_b32(rs, 16 + 4 * kg, 0, 0);
   }
 
-  __device__ __forceinline__ void convert(uint4 (&kr)[2 * KP], uint4 (&vr)[4]) const {
+  // The A fragments of the score products: k-step 2c is the first half of piece c.
+  __device__ __forceinline__ void k_frags(uint4 (&kr)[2 * KP]) const {
     const float f = scale_of<0>(ks);
 #pragma unroll
     for (int c = 0; c < KP; ++c) {
       kr[2 * c] = to_bf16(k[c].x, k[c].y, f);
       kr[2 * c + 1] = to_bf16(k[c].z, k[c].w, f);
     }
-    vr[0] = to_bf16(v[0].x, v[0].y, scale_of<0>(vs));
-    vr[1] = to_bf16(v[0].z, v[0].w, scale_of<1>(vs));
-    vr[2] = to_bf16(v[1].x, v[1].y, scale_of<2>(vs));
-    vr[3] = to_bf16(v[1].z, v[1].w, scale_of<3>(vs));
+  }
+
+  // V's codes and scale bytes become zeros from row `rel` of the lane's four on.
+  __device__ __forceinline__ void clear_v(int rel) {
+    vs = rel <= 0 ? 0u : rel >= 4 ? vs : vs & ((1u << (8 * rel)) - 1);
+    if (rel <= 0) v[0].x = v[0].y = 0u;
+    if (rel <= 1) v[0].z = v[0].w = 0u;
+    if (rel <= 2) v[1].x = v[1].y = 0u;
+    if (rel <= 3) v[1].z = v[1].w = 0u;
   }
 };
 
-// The fold of one block, on converted tiles, into the states of NT tiles of 16
-// rows.  As WaveAttention::process, but each probability is split into three bf16
-// parts, each the top 16 bits of what is left, which together are all of its 24
-// bits: the third costs MFMAs that the wait for memory hides (with two the result
-// was 4.8e-6 of its norm off, ten times what the rest of the arithmetic is).
+// The fold of two blocks into the states of NT tiles of 16 rows, on the layouts of
+// WaveAttention.  Scores and probabilities are its own; P V runs on MFMA
+// f32_16x16x32_bf16 over both blocks at once, and each probability is split into
+// three bf16 parts, each the top 16 bits of what is left, which together are all
+// of its 24 bits: the third costs MFMAs that the wait for memory hides (with two
+// the result was 4.8e-6 of its norm off, ten times what the rest of the arithmetic is).
 template <int D>
 struct Fold : WaveAttention<D> {
   using WA = WaveAttention<D>;
   __device__ __forceinline__ Fold() : WA(0.f) {}
-  struct Parts {
-    shortx4_t p[3];
-  };
 
-  __device__ __forceinline__ Parts parts(const uint4 (&kr)[1][WA::NC], int tok0, int L, bool tail) {
-    float sc[1][4];
-    this->template scores<1>(kr, sc);
+  __device__ __forceinline__ void probabilities(const uint4 (&kr)[2][WA::NC], int tok0, int L, int t_stop, bool tail,
+                                                bf16x8_t (&part)[3]) {
+    float sc[2][4];
+    this->template scores<2>(kr, sc);
     if (tail) {
       asm volatile("");  // a branch: as selects the masking would run on every block
-      const int rel = L - this->lim_off - (tok0 + 4 * this->kg);
+      const int rel = min(L - this->lim_off, t_stop) - (tok0 + 4 * this->kg);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i >= rel) sc[0][i] = WA::kNegInf;
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (kBlockTokens * b + i >= rel) sc[b][i] = WA::kNegInf;
     }
-    const float top = max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], WA::kNegInf);
+    float top = max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]);
+    top = max3(max3(sc[1][1], sc[1][2], sc[1][3]), top, top);
     if (__builtin_amdgcn_ballot_w64(top > this->m_run + WA::kRescaleSlack) != 0) this->rescale(top);
-    float pr[4];
+    float pr[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) pr[i] = exp2_fast(sc[0][i] - this->m_run);
-    this->l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-    Parts f;
+    for (int i = 0; i < 8; ++i) pr[i] = exp2_fast(sc[i / 4][i % 4] - this->m_run);
+    this->l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      unsigned w[2];
+      unsigned w[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) w[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
-      f.p[k] = __builtin_bit_cast(shortx4_t, make_uint2(w[0], w[1]));
+      for (int h = 0; h < 4; ++h) w[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
+      part[k] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pr[i] -= __uint_as_float(__float_as_uint(pr[i]) & 0xffff0000u);
+      for (int i = 0; i < 8; ++i) pr[i] -= __uint_as_float(__float_as_uint(pr[i]) & 0xffff0000u);
     }
-    return f;
-  }
-
-  // The A fragment of output tile t: 4 tokens of one column.
-  __device__ __forceinline__ shortx4_t v_frag(const uint4 (&vr)[4], int t) const {
-    const bool hi = t & 1;
-    return __builtin_bit_cast(shortx4_t,
-                              make_uint2(pack_halves(this->col_dword(vr, 0, t), this->col_dword(vr, 1, t), hi),
-                                         pack_halves(this->col_dword(vr, 2, t), this->col_dword(vr, 3, t), hi)));
   }
 };
 
+// Fold blocks c[0], c[1] (tokens tok0 .. tok0 + 31, those from t_stop on not there).
 template <int D, int NT>
-__device__ __forceinline__ void fold_block(Fold<D> (&wave)[NT], const uint4 (&kr)[1][WaveAttention<D>::NC], uint4 (&vr)[4],
-                                           int tok0, int L, int l_first, int l_vis) {
-  const bool tail = tok0 + kBlockTokens > l_first;  // wavefront-uniform
-  typename Fold<D>::Parts f[NT];
+__device__ __forceinline__ void fold_pair(Fold<D> (&wave)[NT], Codes<D> (&c)[2], int tok0, int L, int l_first, int l_vis,
+                                          int t_stop) {
+  const bool tail = tok0 + 2 * kBlockTokens > min(l_first, t_stop);  // wavefront-uniform
+  uint4 kr[2][WaveAttention<D>::NC];
+  c[0].k_frags(kr[0]);
+  c[1].k_frags(kr[1]);
+  bf16x8_t part[NT][3];
 #pragma unroll
-  for (int x = 0; x < NT; ++x) f[x] = wave[x].parts(kr, tok0, L, tail);
-  wave[0].mask_v(vr, tok0, l_vis, tail);
+  for (int x = 0; x < NT; ++x) wave[x].probabilities(kr, tok0, L, t_stop, tail, part[x]);
+  if (tail) {  // rows that no query row sees, whatever they hold
+    asm volatile("");
 #pragma unroll
-  for (int t = 0; t < WaveAttention<D>::VT; ++t) {
-    const shortx4_t a = wave[0].v_frag(vr, t);
+    for (int b = 0; b < 2; ++b) c[b].clear_v(l_vis - (tok0 + kBlockTokens * b + 4 * wave[0].kg));
+  }
+  // Output tiles 2 dw and 2 dw + 1 take the two columns of dword dw of the rows (WaveAttention::col_dword): two codes.
+  const bool upper = D == 64 && wave[0].n >= 8;
+  float f[2][4];
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
+  for (int b = 0; b < 2; ++b) {
+    f[b][0] = scale_of<0>(c[b].vs), f[b][1] = scale_of<1>(c[b].vs);
+    f[b][2] = scale_of<2>(c[b].vs), f[b][3] = scale_of<3>(c[b].vs);
+  }
 #pragma unroll
-      for (int k = 0; k < 3; ++k) wave[x].o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, f[x].p[k], wave[x].o[t], 0, 0, 0);
+  for (int dw = 0; dw < WaveAttention<D>::VT / 2; ++dw) {
+    unsigned w[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint4& v = c[b].v[e / 2];
+        const unsigned lo = e % 2 ? v.z : v.x, hi = e % 2 ? v.w : v.y;
+        const unsigned codes = D == 64 ? (upper ? hi : lo) : dw < 2 ? lo : hi;
+        const bf16x2_t x = dw % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, f[b][e], true)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, f[b][e], false);
+        w[b][e] = __builtin_bit_cast(unsigned, x);
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x8_t a = __builtin_bit_cast(
+          bf16x8_t, make_uint4(pack_halves(w[0][0], w[0][1], h), pack_halves(w[0][2], w[0][3], h),
+                               pack_halves(w[1][0], w[1][1], h), pack_halves(w[1][2], w[1][3], h)));
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          wave[x].o[2 * dw + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, part[x][k], wave[x].o[2 * dw + h], 0, 0, 0);
+    }
   }
 }
 
@@ -194,27 +226,28 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   const int wj0 = min(j1, j0 + w * per_slice);
   const int wj1 = min(j1, wj0 + per_slice);
   bool bad = false;
-  CD c0, c1;
-  auto fold = [&](const CD& c, int j) {
-    uint4 kr[1][WA::NC], vr[4];
-    c.convert(kr[0], vr);
-    fold_block<D, NT>(wave, kr, vr, j * kBlockTokens, L, l_first, l_vis);
-  };
+  CD c0[2], c1[2];  // two pairs of blocks: one is folded, the next in flight
   for (int jc = wj0; jc < wj1; jc += kWaveSize) {
     const int cn = min(kWaveSize, wj1 - jc);
     const int ids = lane < cn ? table_row[jc + lane] : 0;
-    auto load = [&](CD& c, int i) {
-      c.load(args, kpool, vpool, spool, a.num_kv_heads, __builtin_amdgcn_readlane(ids, min(i, cn - 1)), i < cn, lane, bad);
+    auto load = [&](CD (&c)[2], int i) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        c[x].load(args, kpool, vpool, spool, a.num_kv_heads, __builtin_amdgcn_readlane(ids, min(i + x, cn - 1)), i + x < cn,
+                  lane, bad);
+    };
+    auto fold = [&](CD (&c)[2], int i) {
+      fold_pair<D, NT>(wave, c, (jc + i) * kBlockTokens, L, l_first, l_vis, wj1 * kBlockTokens);
     };
     load(c0, 0);
-    for (int i = 0; i < cn; i += 2) {
-      load(c1, i + 1);
+    for (int i = 0; i < cn; i += 4) {
+      load(c1, i + 2);
       __builtin_amdgcn_sched_barrier(0);
-      fold(c0, jc + i);
-      if (i + 1 >= cn) break;
-      load(c0, i + 2);
+      fold(c0, i);
+      if (i + 2 >= cn) break;
+      load(c0, i + 4);
       __builtin_amdgcn_sched_barrier(0);
-      fold(c1, jc + i + 1);
+      fold(c1, i + 2);
     }
   }
 

@@ -34,7 +34,6 @@ constexpr int kTileRows = 32;      // query rows of a wavefront
 constexpr int kStageBlocks = 2;    // blocks of a step: 32 tokens
 constexpr int kBuffers = 3;
 constexpr int kWindow = 1024;      // block ids held in LDS at a time
-constexpr float kExactMax = 128.f; // running maxima whose rounding is below P's resolution
 
 template <int D, int W>
 struct WideLds {
@@ -122,12 +121,11 @@ wide_fp8_kernel(const DecodeFp8Args args) {
   for (int t = 0; t < VT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  // The running maximum before scaling, and scaled and rounded.  A step that
-  // moves the maximum takes its probabilities as exp2((s - m_raw) * scale), so the
-  // row's largest score gets exactly 1 and scores of any size cancel; the others take
-  // them as exp2(s * scale - m_run), in one instruction less per score, as long as
-  // the rounding of m_run (up to kExactMax: below 2^-17) is all that differs.
-  float m_raw = fmaxf(-1e30f / scale, -__FLT_MAX__), m_run = mul_rounded(m_raw, scale), l_run = 0.f;
+  // The reference of a row's probabilities, exp2(s * scale - m_run): a whole number
+  // at most 8 below the largest scaled score so far (nothing overflows, and nothing
+  // that counts underflows).  The difference is one fused operation on an exact
+  // reference, so scores of any size cancel.
+  float m_run = -1e30f, l_run = 0.f;
 
   const int32_t* table_row = a.table + (size_t)b * a.max_blocks_per_seq;
   const int J0 = p * Tp / kBlockTokens;
@@ -176,8 +174,11 @@ wide_fp8_kernel(const DecodeFp8Args args) {
       const uint8_t* pool = side_of(k) == 0 ? args.k : args.v;
       const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(tile_rsrc(pool + tile * kTile, kTile), g_off[k], 0, 0);
       raw[k] = make_uint4(t[0], t[1], t[2], t[3]);
-      // (two bytes, of which a K piece uses the first: past the last slot it reads V's first byte)
-      raw_scale[k] = __builtin_amdgcn_raw_buffer_load_b16(tile_rsrc(args.scale + tile * 32, 32), s_off[k], 0, 0);
+      const __amdgpu_buffer_rsrc_t rs = tile_rsrc(args.scale + tile * 32, 32);
+      if (side_of(k) == 0)
+        raw_scale[k] = __builtin_amdgcn_raw_buffer_load_b8(rs, s_off[k], 0, 0);
+      else
+        raw_scale[k] = __builtin_amdgcn_raw_buffer_load_b16(rs, s_off[k], 0, 0);
     }
   };
   auto commit = [&](uint4* buf, int tok0) {
@@ -252,15 +253,10 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int t = 0; t < VT; ++t) vf[m][t] = v_frag(m, t);
-    float ref = m_run;
-    if (__builtin_amdgcn_ballot_w64(fmaf(top, scale, -m_run) > 8.f || fabsf(m_run) > kExactMax) != 0) {
-      const float mn = fmaxf(m_raw, fmaxf(top, __shfl_xor(top, 32)));
-      const float al = exp2_fast((m_raw - mn) * scale);
-      m_raw = mn;
-      m_run = mul_rounded(mn, scale);
-      ref = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] -= m_raw;
+    if (__builtin_amdgcn_ballot_w64(fmaf(top, scale, -m_run) > 8.f) != 0) {
+      const float m_new = fmaxf(m_run, __builtin_ceilf(mul_rounded(fmaxf(top, __shfl_xor(top, 32)), scale)));
+      const float al = exp2_fast(m_run - m_new);
+      m_run = m_new;
       l_run *= al;
 #pragma unroll
       for (int t = 0; t < VT; ++t) o[t] *= al;
@@ -273,13 +269,14 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     for (int m = 0; m < 2; ++m) {
       float pr[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pr[i] = exp2_fast(fmaf(s[8 * m + i], scale, -ref));
+      for (int i = 0; i < 8; ++i) pr[i] = exp2_fast(fmaf(s[8 * m + i], scale, -m_run));
       l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
       unsigned hw[4], lw[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const bf16x2_t h2 = {(__bf16)pr[2 * h], (__bf16)pr[2 * h + 1]};
         hw[h] = __builtin_bit_cast(unsigned, h2);
+        asm("" : "+v"(hw[h]));  // (one conversion for both uses)
         const bf16x2_t l2 = {(__bf16)(pr[2 * h] - __uint_as_float(hw[h] << 16)),
                              (__bf16)(pr[2 * h + 1] - __uint_as_float(hw[h] & 0xffff0000u))};
         lw[h] = __builtin_bit_cast(unsigned, l2);

@@ -116,4 +116,60 @@ __device__ __forceinline__ float2 turn(const RotaryArgs& r, int position, int pa
   return make_float2(c * r.magnitude, r.sign * s * r.magnitude);
 }
 
+// A thread's share of a head row: two vectors of 8 elements, d0 and d1 (from D on:
+// there is none), of which the first `turned` are rotated.  In the half layout a
+// rotated share is 8 pairs; interleaved, each vector is 4 pairs by itself.  Shares of
+// neighbouring threads are neighbouring vectors, so that a store of the
+// wavefront covers whole cache lines where the row allows it.
+struct RowShare {
+  int d0, d1, turned;
+};
+__host__ __device__ constexpr int row_shares(int head_dim) { return (head_dim + 15) / 16; }
+__device__ __forceinline__ RowShare row_share(const RotaryArgs& r, int rotary_dim, int head_dim, int u) {
+  const int shares = row_shares(head_dim);
+  if (r.interleaved || rotary_dim == 0) {
+    const int d0 = 8 * u, d1 = 8 * (u + shares);
+    return RowShare{d0, d1, d1 < rotary_dim ? 2 : d0 < rotary_dim ? 1 : 0};
+  }
+  const int pairs8 = rotary_dim / 16;
+  if (u < pairs8) return RowShare{8 * u, rotary_dim / 2 + 8 * u, 2};
+  const int d0 = rotary_dim + 8 * (u - pairs8);
+  return RowShare{d0, d0 + 8 * (shares - pairs8), 0};
+}
+
+// Rotates a share's vectors by the cosines and sines of the row's pairs.
+__device__ __forceinline__ void rotate_share(const float2* turns, bool interleaved, const RowShare& w, float (&p)[8],
+                                             float (&q)[8]) {
+  auto four = [](const float2* cs, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float2 c = cs[e / 2];
+      const float a = x[e], b = x[e + 1];
+      x[e] = a * c.x - b * c.y, x[e + 1] = b * c.x + a * c.y;
+    }
+  };
+  if (w.turned == 0) return;
+  if (interleaved) {
+    four(turns + w.d0 / 2, p);
+    if (w.turned == 2) four(turns + w.d1 / 2, q);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 c = turns[w.d0 + e];
+      const float a = p[e], b = q[e];
+      p[e] = a * c.x - b * c.y, q[e] = b * c.x + a * c.y;
+    }
+  }
+}
+
+// Whether the stores of the rotated rows (bf16) cover whole cache lines of 128 bytes:
+// then, with many tokens, they go out with the non-temporal hint (16384 tokens of
+// 32 + 8 heads of 128: 57 -> 48 us); lines written in halves would be written
+// twice (neighbouring pairs in shares of 16 neighbouring elements: 44 -> 57 us).
+inline bool whole_lines(const RotaryArgs& r, int head_dim) {
+  const int copied = r.interleaved ? head_dim : head_dim - r.rotary_dim;  // elements in vectors of their own
+  return copied % 128 == 0 && (r.interleaved || r.rotary_dim % 128 == 0);
+}
+constexpr int64_t kManyTokens = 2048;
+
 }  // namespace pda

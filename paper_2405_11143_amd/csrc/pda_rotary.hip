@@ -3,15 +3,17 @@
 // Bound by memory: every row is read and written once, and a pair costs 4
 // multiply-adds.  The angles are what is expensive (a 64-bit product and
 // reduction, then sine and cosine), and the same for all heads of a token: a
-// workgroup takes one or a few tokens, forms their cosines and sines in LDS
-// first, one thread each, and then streams the tokens' rows, 16 elements per
-// thread: 8 pairs, as two vectors of 8 in either layout.
+// workgroup takes one token, forms its cosines and sines in LDS, a thread each,
+// and then its rows, 16 elements per thread.  16384 tokens of 32 + 8 heads of 128, bf16:
+// 48 us, 6.8 TB/s; neighbouring pairs in half of 28 + 4 heads' elements, the
+// others copied: 39 us, 6.8 TB/s.  Four tokens to a workgroup (its loop goes from row
+// to row and from token to token) took 63 us where one took 58, two 64.
 #include "pda_fp8_internal.h"
 
 namespace pda {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kMaxThreads = 256;
 constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
 constexpr int kMaxPairs = 256;  // head_dim <= 512
 
@@ -29,83 +31,70 @@ __device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
 }
+template <bool NT>
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
+template <bool NT>
 __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
   v8 a;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = (__bf16)x[i];
-  *reinterpret_cast<v8*>(p) = a;
+  if (NT)
+    __builtin_nontemporal_store(a, reinterpret_cast<v8*>(p));
+  else
+    *reinterpret_cast<v8*>(p) = a;
 }
 
-// TOKENS: tokens of a workgroup.
-template <typename T, int TOKENS>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryApplyArgs a) {
-  __shared__ float2 turns[TOKENS][kMaxPairs];
-  const int R = a.rot.rotary_dim;
-  const int pairs = R / 2;
-  for (int64_t t0 = (int64_t)blockIdx.x * TOKENS; t0 < a.num_tokens; t0 += (int64_t)gridDim.x * TOKENS) {
-  const int nt = (int)min((int64_t)TOKENS, a.num_tokens - t0);
-  for (int x = threadIdx.x; x < nt * pairs; x += kThreads) {
-    const int pos = a.positions[t0 + x / pairs];
-    if (pos >= 0) turns[x / pairs][x % pairs] = turn(a.rot, pos, x % pairs);
-  }
-  __syncthreads();
-  const int units = R / 16;                           // of 8 pairs
-  const int per_head = units + (a.head_dim - R) / 8;  // and vectors of 8 that are copied
+// NT: stores with the non-temporal hint.
+template <typename T, bool NT>
+__global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const RotaryApplyArgs a) {
+  __shared__ float2 turns[kMaxPairs];
+  const int D = a.head_dim;
+  const int pairs = a.rot.rotary_dim / 2;
+  const int shares = row_shares(D);
+  const int first_row = threadIdx.x / shares;
+  const int rows_at_once = blockDim.x / shares;
+  const RowShare w = row_share(a.rot, a.rot.rotary_dim, D, threadIdx.x % shares);
   const int heads = a.q.heads + a.k.heads;
-  for (int x = threadIdx.x; x < nt * heads * per_head; x += kThreads) {
-    const int u = x % per_head;
-    const int hx = x / per_head % heads;
-    const int t = x / per_head / heads;
-    if (a.positions[t0 + t] < 0) continue;
-    const bool is_q = hx < a.q.heads;
-    const RotaryRows& r = is_q ? a.q : a.k;
-    const int h = is_q ? hx : hx - a.q.heads;
-    const T* in = static_cast<const T*>(r.in) + (int64_t)(t0 + t) * r.in_stride + (int64_t)h * a.head_dim;
-    T* out = static_cast<T*>(r.out) + (int64_t)(t0 + t) * r.out_stride + (int64_t)h * a.head_dim;
-    float p[8], q[8];
-    if (u >= units) {
-      const int d = R + 8 * (u - units);
-      if (r.in == r.out) continue;
-      load8(in + d, p);
-      store8(out + d, p);
-      continue;
+  for (int t = blockIdx.x; t < a.num_tokens; t += gridDim.x) {
+    const int pos = a.positions[t];
+    if (pos < 0) continue;  // padding (the whole workgroup)
+    for (int x = threadIdx.x; x < pairs; x += blockDim.x) turns[x] = turn(a.rot, pos, x);
+    __syncthreads();
+    for (int h = first_row < rows_at_once ? first_row : heads; h < heads; h += rows_at_once) {
+      const bool is_q = h < a.q.heads;
+      const RotaryRows& r = is_q ? a.q : a.k;
+      const int64_t at = (int64_t)(is_q ? h : h - a.q.heads) * D;
+      const T* in = static_cast<const T*>(r.in) + t * r.in_stride + at;
+      T* out = static_cast<T*>(r.out) + t * r.out_stride + at;
+      const bool copies = r.in != r.out;
+      const bool one = copies || w.turned > 0, two = w.d1 < D && (copies || w.turned > 1);
+      float p[8], q[8];
+      if (one) load8(in + w.d0, p);
+      if (two) load8(in + w.d1, q);
+      rotate_share(turns, a.rot.interleaved, w, p, q);
+      if (one) store8<NT>(out + w.d0, p);
+      if (two) store8<NT>(out + w.d1, q);
     }
-    const int d0 = a.rot.interleaved ? 16 * u : 8 * u;
-    const int d1 = a.rot.interleaved ? d0 + 8 : d0 + pairs;
-    load8(in + d0, p);
-    load8(in + d1, q);
-    const float2* cs = &turns[t][8 * u];
-    if (a.rot.interleaved) {
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float2 c0 = cs[i / 2], c1 = cs[4 + i / 2];
-        const float x0 = p[i], y0 = p[i + 1], x1 = q[i], y1 = q[i + 1];
-        p[i] = x0 * c0.x - y0 * c0.y, p[i + 1] = y0 * c0.x + x0 * c0.y;
-        q[i] = x1 * c1.x - y1 * c1.y, q[i + 1] = y1 * c1.x + x1 * c1.y;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 c = cs[i];
-        const float x0 = p[i], y0 = q[i];
-        p[i] = x0 * c.x - y0 * c.y, q[i] = y0 * c.x + x0 * c.y;
-      }
-    }
-    store8(out + d0, p);
-    store8(out + d1, q);
-  }
-  __syncthreads();  // the next tokens' turns take the same place
+    __syncthreads();  // the next token's turns take the same place
   }
 }
 
+// A workgroup has as many threads as make its last trip through the rows a full
+// one, nearly (up to 512 of them for a single trip: 65 us against 58).
 template <typename T>
 hipError_t launch_t(const RotaryApplyArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((rotary_kernel<T, 1>), dim3(min(a.num_tokens, kMaxGrid)), dim3(kThreads), 0, stream, a);
+  const int units = (a.q.heads + a.k.heads) * row_shares(a.head_dim);
+  const int trips = (units + kMaxThreads - 1) / kMaxThreads;
+  const int threads = min(kMaxThreads, ((units + trips - 1) / trips + kWaveSize - 1) / kWaveSize * kWaveSize);
+  const dim3 grid(min(a.num_tokens, kMaxGrid));
+  if (sizeof(T) == 2 && a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim))
+    hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(threads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(threads), 0, stream, a);
   return hipGetLastError();
 }
 

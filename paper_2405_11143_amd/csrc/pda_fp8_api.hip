@@ -11,6 +11,21 @@
 namespace {
 
 constexpr int64_t kAtOnce = 768;  // workgroups the GPU runs at once: 3 per compute unit
+// Ordered steps of at most this many items, and of pda::kPickPairs pairs, find their
+// items without the order kernel: a step of 256 sequences of 512-4096 tokens (2048 items)
+// takes 194.7 us instead of 197.7, 8 of up to 16384 (1152) 21.4 instead of 23.3.  Ranking costs
+// every workgroup about a microsecond: 16 of up to 16384 in 512s (3328 items) took
+// 42.5 instead of 36.7.
+constexpr int64_t kPickItems = 3 * kAtOnce;
+// Contexts up to this length stay whole where they all run at once and there are
+// kWholePairs (sequence, KV head) pairs for every kWholeOf tokens: a workgroup alone on a
+// compute unit reads 2048 tokens in 13 us, and splitting costs a merge of 5, which
+// pays where most compute units would be idle.  Whole / the best of 256, 512 and 1024 in
+// us, 8 KV heads, contexts uniform up to the maximum: 24 sequences of 2048 16.6 / 17.8, 16
+// 16.8 / 13.9, 16 of 1500 13.6 / 13.4, 24 13.8 / 15.8, 16 of 1024 10.5 / 11.1, 8 10.5 /
+// 9.5; 64 of 2048 31.8 / 30.0, 48 26.4 / 25.7.
+constexpr int kWholeTokens = 2048;
+constexpr int64_t kWholePairs = 1, kWholeOf = 12;
 constexpr int64_t kMostItems = (1 << 24) - 1;  // workgroups of 256: a launch has less than 2^32 threads
 constexpr int kMaxHeadDim = 512;  // of pda_rotary_apply
 
@@ -44,15 +59,25 @@ struct Plan {
   int tiles;      // row tiles of a sequence and KV head
   int64_t items;  // partitions x sequences x KV heads x tiles
   size_t slots;   // partial states, 0 when nothing is split
+  bool narrow;    // few query rows: the decode kernel
 };
 
 int make_plan(const pda_problem* p, Plan* plan) {
   int rc = pda_plan(p, &plan->info);
   if (rc != PDA_OK) return rc;
   const int n = query_tokens(p);
+  if (p->partition_tokens == 0 && (int64_t)n * (p->num_q_heads / p->num_kv_heads) <= pda::kFp8TileRows &&
+      p->max_context_len <= kWholeTokens && (int64_t)p->num_seqs * p->num_kv_heads <= kAtOnce &&
+      (int64_t)p->num_seqs * p->num_kv_heads * kWholeOf >= kWholePairs * p->max_context_len) {
+    pda_problem whole = *p;
+    whole.partition_tokens = kWholeTokens;
+    rc = pda_plan(&whole, &plan->info);
+    if (rc != PDA_OK) return rc;
+  }
   const int64_t rows = (int64_t)n * (p->num_q_heads / p->num_kv_heads);
   const int item_rows = pda::fp8_item_rows(rows);
   plan->tiles = (int)((rows + item_rows - 1) / item_rows);
+  plan->narrow = item_rows <= 2 * pda::kFp8TileRows;
   const int64_t parts = plan->info.num_partitions;
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
   const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads * plan->tiles;
@@ -213,7 +238,9 @@ int pda_decode_fp8(const pda_problem* prob, const void* q, const void* k_cache, 
   }
   // when every item runs at once their order is irrelevant (and the grid's y and z must hold them)
   const bool ordered = plan.items > kAtOnce;
-  if (ordered) s.order = reinterpret_cast<int32_t*>(ws + plan.slots * (prob->head_dim + 2));
+  a.picks = ordered && plan.narrow && plan.items <= kPickItems &&
+            (int64_t)prob->num_seqs * plan.info.num_partitions <= pda::kPickPairs;
+  if (ordered && !a.picks) s.order = reinterpret_cast<int32_t*>(ws + plan.slots * (prob->head_dim + 2));
   s.q = static_cast<const uint16_t*>(q);
   s.table = block_table;
   s.lens = context_lens;
@@ -239,7 +266,7 @@ int pda_decode_fp8(const pda_problem* prob, const void* q, const void* k_cache, 
   a.k = static_cast<const uint8_t*>(k_cache);
   a.v = static_cast<const uint8_t*>(v_cache);
   a.scale = kv_scale;
-  if (ordered && pda::launch_order(s, stream) != hipSuccess) return PDA_ERR_HIP;
+  if (s.order && pda::launch_order(s, stream) != hipSuccess) return PDA_ERR_HIP;
   if (pda::launch_decode_fp8(a, prob->head_dim, stream) != hipSuccess) return PDA_ERR_HIP;
   if (plan.slots > 0 && pda::launch_merge(s, prob->head_dim, stream) != hipSuccess) return PDA_ERR_HIP;
   return PDA_OK;

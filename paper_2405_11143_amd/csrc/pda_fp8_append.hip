@@ -153,7 +153,7 @@ template <int D>
 hipError_t launch_d(const AppendFp8Args& a, hipStream_t stream) {
   const int units = ((a.q ? a.num_q_heads : 0) + 2 * a.num_kv_heads) * (D / 16);
   auto launch = [&](auto kernel, int tokens) {
-    const int groups = (a.num_query_tokens + tokens - 1) / tokens;
+    const int groups = (a.num_query_tokens - 1) / tokens + 1;
     const unsigned grid = (unsigned)min((int64_t)a.num_seqs * groups, kMaxGrid);
     // as many threads as make the last trip through the rows a full one, nearly
     const int64_t all = (int64_t)tokens * units;

@@ -26,6 +26,63 @@ struct DecodeShared {
   int bad[kWaves];
 };
 
+// The work order (pda_order.hip: largest partition first, placed for the XCDs)
+// without its kernel, whose launch is 5 us of a step: each workgroup ranks the
+// (sequence, partition) pairs, one per thread, by a counting sort in LDS of which
+// it needs one place only.  Pairs of one size class stay in the order of their indexes.
+struct PickShared {
+  int count[kOrderBuckets];  // pairs of a size class, largest first
+  int found[2];              // the class that holds the place, and the place in it
+  int waves[kWaves];         // pairs of that class in each wavefront
+  int pair;
+};
+
+// The pair at place `pos`.  All threads of the workgroup call this.
+__device__ __forceinline__ int pick_pair(const StepArgs& a, int pos, PickShared& s) {
+  static_assert(kOrderBuckets == kThreads && kPickPairs == kThreads, "a class and a pair per thread");
+  const int tid = threadIdx.x, lane = tid & (kWaveSize - 1), w = tid / kWaveSize;
+  s.count[tid] = 0;
+  int cls = -1;
+  if (tid < a.num_seqs * a.num_partitions) {
+    const int p = tid / a.num_seqs;
+    const int L = clamped(a.lens[tid - p * a.num_seqs], a.max_context_len);
+    const int tok = min(max(L - p * a.partition_tokens, 0), a.partition_tokens);
+    cls = kOrderBuckets - 1 - min((tok + kBlockTokens - 1) / kBlockTokens, kOrderBuckets - 1);
+  }
+  __syncthreads();
+  if (cls >= 0) atomicAdd(&s.count[cls], 1);
+  __syncthreads();
+  if (w == 0) {
+    constexpr int kPer = kOrderBuckets / kWaveSize;
+    int v[kPer], sum = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) v[e] = s.count[kPer * lane + e], sum += v[e];
+    int before = sum;  // inclusive scan over the lanes, then exclusive
+#pragma unroll
+    for (int o = 1; o < kWaveSize; o <<= 1) {
+      const int t = __shfl_up(before, o);
+      if (lane >= o) before += t;
+    }
+    before -= sum;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (pos >= before && pos < before + v[e]) s.found[0] = kPer * lane + e, s.found[1] = pos - before;
+      before += v[e];
+    }
+  }
+  __syncthreads();
+  const uint64_t hits = __builtin_amdgcn_ballot_w64(cls == s.found[0]);
+  if (lane == 0) s.waves[w] = __builtin_popcountll(hits);
+  __syncthreads();
+  int left = s.found[1];  // matches before the one that is wanted
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x)
+    if (x < w) left -= s.waves[x];
+  if ((hits >> lane & 1) && left == __builtin_popcountll(hits & ((uint64_t(1) << lane) - 1))) s.pair = tid;
+  __syncthreads();
+  return s.pair;
+}
+
 // One block's codes and scale bytes in a lane's registers.
 template <int D>
 struct Codes {
@@ -178,7 +235,11 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(N
 decode_fp8_kernel(const DecodeFp8Args args) {
   using WA = WaveAttention<D>;
   using CD = Codes<D>;
-  __shared__ __align__(16) DecodeShared<D, NT * kFp8TileRows> sh;
+  __shared__ __align__(16) union {
+    DecodeShared<D, NT * kFp8TileRows> sh;  // the epilogue
+    PickShared pick;
+  } lds;
+  DecodeShared<D, NT * kFp8TileRows>& sh = lds.sh;
   const StepArgs& a = args.step;
   const int tiles = a.num_chunk_groups;
   int gt, b, p;  // KV head and tile, sequence, partition
@@ -187,6 +248,22 @@ decode_fp8_kernel(const DecodeFp8Args args) {
     if ((unsigned)item >= (unsigned)a.num_regular_items) return;
     const int HC = a.num_kv_heads * tiles;
     gt = item % HC, b = item / HC % a.num_seqs, p = item / (HC * a.num_seqs);
+  } else if (args.picks) {  // the places of pda_order.hip
+    const int H = a.num_kv_heads, HC = H * tiles, pairs = a.num_seqs * a.num_partitions;
+    const int slot = blockIdx.x;
+    int pos, x;
+    if (H % 8 == 0) {
+      pos = slot / HC;
+      x = slot % HC;
+      gt = x % H * tiles + x / H;
+    } else {
+      const int first = slot / (8 * HC) * 8, c = min(8, pairs - first);
+      const int in = slot - first * HC;
+      pos = first + in % c;
+      gt = in / c;
+    }
+    const int pair = __builtin_amdgcn_readfirstlane(pick_pair(a, pos, lds.pick));  // (the epilogue's LDS: barriers between)
+    p = pair / a.num_seqs, b = pair % a.num_seqs;
   } else {
     gt = blockIdx.x, b = blockIdx.y, p = blockIdx.z;
   }
@@ -314,7 +391,7 @@ template <int D>
 hipError_t launch_d(const DecodeFp8Args& a, hipStream_t stream) {
   const StepArgs& s = a.step;
   if (s.num_query_tokens * s.group > 2 * kFp8TileRows) return launch_wide_fp8(a, D, stream);
-  const dim3 grid = s.order ? dim3((unsigned)s.num_regular_items)
+  const dim3 grid = s.order || a.picks ? dim3((unsigned)s.num_regular_items)
                             : dim3((unsigned)s.num_kv_heads * (unsigned)s.num_chunk_groups, s.num_seqs, s.num_partitions);
   if (s.num_query_tokens * s.group <= kFp8TileRows)
     hipLaunchKernelGGL((decode_fp8_kernel<D, 1>), grid, dim3(kThreads), 0, stream, a);

@@ -55,7 +55,10 @@ struct DecodeFp8Args {
   const uint8_t* k;        // e4m3 [num_blocks][Hkv][D/64][4][16][2][8]
   const uint8_t* v;        // e4m3 [num_blocks][Hkv][2][4][D/8][2][8]
   const uint8_t* scale;    // [num_blocks][Hkv][2][16]
+  bool picks;              // every workgroup finds its item in the work order by itself (no step.order)
 };
+
+constexpr int kPickPairs = 256;  // (sequence, partition) pairs of a step that does: one per thread
 
 struct ReadFp8Args {
   const uint8_t* k;

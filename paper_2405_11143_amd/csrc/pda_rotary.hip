@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const RotaryApplyAr
   const int rows_at_once = blockDim.x / shares;
   const RowShare w = row_share(a.rot, a.rot.rotary_dim, D, threadIdx.x % shares);
   const int heads = a.q.heads + a.k.heads;
-  for (int t = blockIdx.x; t < a.num_tokens; t += gridDim.x) {
+  for (int64_t t = blockIdx.x; t < a.num_tokens; t += gridDim.x) {
     const int pos = a.positions[t];
     if (pos < 0) continue;  // padding (the whole workgroup)
     for (int x = threadIdx.x; x < pairs; x += blockDim.x) turns[x] = turn(a.rot, pos, x);

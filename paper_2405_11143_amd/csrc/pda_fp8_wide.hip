@@ -32,18 +32,22 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kTileRows = 32;      // query rows of a wavefront
 constexpr int kStageBlocks = 2;    // blocks of a step: 32 tokens
-constexpr int kBuffers = 3;
-constexpr int kWindow = 1024;      // block ids held in LDS at a time
+
+// Two-wavefront workgroups form their scores in the step itself, with two buffers
+// instead of three, so that four of them fit a compute unit instead of three.
+constexpr bool scores_ahead(int W) { return W == 4; }
+constexpr int buffers(int W) { return scores_ahead(W) ? 3 : 2; }
+constexpr int window(int W) { return W == 4 ? 1024 : 256; }  // block ids held in LDS at a time
 
 template <int D, int W>
 struct WideLds {
   static constexpr int kTilePieces = 2 * D;  // 16-byte pieces of a bf16 K or V tile
   static constexpr int kBlockPieces = 2 * kTilePieces;
   union {
-    uint4 buf[kBuffers][kStageBlocks][kBlockPieces];
+    uint4 buf[buffers(W)][kStageBlocks][kBlockPieces];
     f32x4_t o[W][kTileRows][D / 8];  // the epilogue, half of the columns at a time
   };
-  int ids[kWindow];
+  int ids[window(W)];
 };
 
 template <int D, int W>
@@ -51,6 +55,8 @@ __global__ void __launch_bounds__(W * kWaveSize) __attribute__((amdgpu_waves_per
 wide_fp8_kernel(const DecodeFp8Args args) {
   using S = WideLds<D, W>;
   constexpr int kThreads = W * kWaveSize;
+  constexpr int kBuffers = buffers(W), kWindow = window(W);
+  constexpr bool kAhead = scores_ahead(W);
   constexpr int KS = D / 16;  // score MFMA k-steps
   constexpr int VT = D / 32;  // output tiles of 32 columns
   constexpr int RP = D / 8;   // 16-byte pieces of a bf16 V row
@@ -242,6 +248,11 @@ wide_fp8_kernel(const DecodeFp8Args args) {
   // Fold the step whose scores are in s (two blocks of a buffer), and form the
   // scores of the next one (in next_blocks).
   auto fold = [&](int tok0, const uint4* blocks, const uint4* next_blocks) {
+    if constexpr (!kAhead) {
+      s = scores(blocks);
+      largest();
+      mask(tok0);
+    }
     auto v_frag = [&](int m, int t) {
       const uint16_t* v0 = reinterpret_cast<const uint16_t*>(blocks + S::kTilePieces + m * S::kBlockPieces) + tr_off[t];
       const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)v0));
@@ -261,7 +272,8 @@ wide_fp8_kernel(const DecodeFp8Args args) {
 #pragma unroll
       for (int t = 0; t < VT; ++t) o[t] *= al;
     }
-    const f32x16_t ns = scores(next_blocks);
+    f32x16_t ns;
+    if constexpr (kAhead) ns = scores(next_blocks);
     // Each probability as two bf16 halves, both rounded to nearest: hi = bf16(p), lo
     // = bf16(p - hi), at most 2^-18 of p off.
     bf16x8_t bh[2], bl[2];
@@ -292,9 +304,11 @@ wide_fp8_kernel(const DecodeFp8Args args) {
         o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bh[m], o[t], 0, 0, 0);
         o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bl[m], o[t], 0, 0, 0);
       }
-    s = ns;
-    largest();
-    mask(tok0 + 32);
+    if constexpr (kAhead) {
+      s = ns;
+      largest();
+      mask(tok0 + 32);
+    }
   };
 
   for (int jw = J0; jw < J1; jw += kWindow) {
@@ -309,15 +323,16 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     }
     __syncthreads();
     const int tok_w = jw * kBlockTokens;
+    constexpr int kStaged = kBuffers - 1;  // steps written before they are folded
 #pragma unroll
-    for (int x = 0; x < kBuffers - 1; ++x)
+    for (int x = 0; x < kStaged; ++x)
       if (x < nsteps) {
         issue(x);
         commit(st.buf[x][0], tok_w + 32 * x);
       }
-    if (kBuffers - 1 < nsteps) issue(kBuffers - 1);
+    if (kStaged < nsteps) issue(kStaged);
     __syncthreads();
-    if (active) {
+    if (kAhead && active) {
       s = scores(st.buf[0][0]);
       largest();
       mask(tok_w);
@@ -326,17 +341,18 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     // addresses: the loop is unrolled by the buffers).  False at the last step.
     auto one = [&](auto B, int step) {
       const int tok0 = tok_w + 32 * step;
-      // behind the barrier the last step's buffer is free, and the next step's written
+      // behind the barrier the last step's buffer is free, and what this step reads is written
       if (step > 0) __syncthreads();
-      if (step + 2 < nsteps) commit(st.buf[(B + 2) % kBuffers][0], tok0 + 64);
-      if (step + 3 < nsteps) issue(step + 3);
+      if (step + kStaged < nsteps) commit(st.buf[(B + kStaged) % kBuffers][0], tok0 + 32 * kStaged);
+      if (step + kBuffers < nsteps) issue(step + kBuffers);
       if (active && tok0 < l_vis) fold(tok0, st.buf[B][0], st.buf[(B + 1) % kBuffers][0]);  // wavefront-uniform
       return step + 1 < nsteps;
     };
     for (int step = 0;; step += kBuffers) {
       if (!one(std::integral_constant<int, 0>{}, step)) break;
       if (!one(std::integral_constant<int, 1>{}, step + 1)) break;
-      if (!one(std::integral_constant<int, 2>{}, step + 2)) break;
+      if constexpr (kBuffers == 3)
+        if (!one(std::integral_constant<int, 2>{}, step + 2)) break;
     }
     __syncthreads();
   }

@@ -1,15 +1,20 @@
-// Pass 1 of attention over the 8-bit KV cache (include/pda_fp8.h); the order and
-// merge kernels are those of the bf16 cache.
+// Pass 1 of attention over the 8-bit KV cache (include/pda_fp8.h) for up to 32
+// query rows per sequence and KV head: decode steps and the verification of a few
+// drafted tokens.  The merge kernel is that of the bf16 cache, and so is the order
+// kernel of steps with many items.
 //
-// A work item is (partition of a context, sequence, KV head, tile of 16 query
-// rows): row r of a sequence and KV head is head r % G of its new token r / G.  The
-// 4 wavefronts of a workgroup take contiguous runs of the partition's blocks;
-// each streams them through registers and folds them with WaveAttention
-// (pda_wave.h), whose lanes want exactly what the layouts give: a 16-byte K
-// piece is the lane's A fragments of two k-steps, a V piece its 8 columns of
-// two of its four tokens.  Codes become bf16 in registers, two per instruction,
-// the row's power of two applied by the same instruction, so what is
-// folded is what a bf16 cache of the stored values would hold.
+// A work item is (partition of a context, sequence, KV head): row r is head r % G of
+// its new token r / G.  Bound by HBM: 2 D + 2 bytes per token and KV head, 256 flop
+// each for every row (D = 128).  The 4 wavefronts of a workgroup take contiguous
+// runs of the partition's blocks; each streams them through registers, two blocks
+// folded while two are in flight, on the layouts of WaveAttention (pda_wave.h), whose
+// lanes want exactly what the cache gives: a 16-byte K piece is the lane's A
+// fragments of two k-steps, a V piece its 8 columns of two of its four tokens.  Codes
+// become bf16 in registers, two per instruction, the row's power of two applied by the
+// same instruction, so what is folded is what a bf16 cache of the stored values would
+// hold.  256 sequences of 512-4096 tokens, 32 / 8 heads of 128: 195 us, 6.3 TB/s (a bare
+// gather of the same tiles takes 180); 5 new tokens each 218 us.  Three and four pairs of
+// blocks in flight changed nothing (198): a wavefront has 3 neighbours on its SIMD.
 #include "pda_fp8_internal.h"
 #include "pda_wave.h"
 
@@ -241,48 +246,46 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   } lds;
   DecodeShared<D, NT * kFp8TileRows>& sh = lds.sh;
   const StepArgs& a = args.step;
-  const int tiles = a.num_chunk_groups;
-  int gt, b, p;  // KV head and tile, sequence, partition
+  int g, b, p;  // KV head, sequence, partition
   if (a.order) {
     const int item = a.order[blockIdx.x];
     if ((unsigned)item >= (unsigned)a.num_regular_items) return;
-    const int HC = a.num_kv_heads * tiles;
-    gt = item % HC, b = item / HC % a.num_seqs, p = item / (HC * a.num_seqs);
+    const int H = a.num_kv_heads;
+    g = item % H, b = item / H % a.num_seqs, p = item / (H * a.num_seqs);
   } else if (args.picks) {  // the places of pda_order.hip
-    const int H = a.num_kv_heads, HC = H * tiles, pairs = a.num_seqs * a.num_partitions;
+    const int H = a.num_kv_heads;
     const int slot = blockIdx.x;
-    int pos, x;
+    int pos;
     if (H % 8 == 0) {
-      pos = slot / HC;
-      x = slot % HC;
-      gt = x % H * tiles + x / H;
+      pos = slot / H, g = slot % H;
     } else {
-      const int first = slot / (8 * HC) * 8, c = min(8, pairs - first);
-      const int in = slot - first * HC;
-      pos = first + in % c;
-      gt = in / c;
+      const int first = slot / (8 * H) * 8, c = min(8, a.num_seqs * a.num_partitions - first);
+      const int in = slot - first * H;
+      pos = first + in % c, g = in / c;
     }
     const int pair = __builtin_amdgcn_readfirstlane(pick_pair(a, pos, lds.pick));  // (the epilogue's LDS: barriers between)
     p = pair / a.num_seqs, b = pair % a.num_seqs;
   } else {
-    gt = blockIdx.x, b = blockIdx.y, p = blockIdx.z;
+    g = blockIdx.x, b = blockIdx.y, p = blockIdx.z;
   }
-  const int g = gt / tiles, tile = gt % tiles;
   const int G = a.group, n = a.num_query_tokens, Hq = a.num_q_heads, Tp = a.partition_tokens;
   const int tid = threadIdx.x;
   const int lane = tid & (kWaveSize - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int L = clamped(a.lens[b], a.max_context_len);
 
-  const int r0 = tile * (NT * kFp8TileRows);
-  const int rows = min(NT * kFp8TileRows, n * G - r0);
-  auto limit_of = [&](int r) { return L - n + 1 + r / G; };  // row r sees tokens below it
-  auto out_row = [&](int r) { return ((size_t)b * n + r / G) * Hq + (size_t)g * G + r % G; };
-  const int l_first = limit_of(r0);
-  const int l_vis = limit_of(r0 + rows - 1);
+  const int rows = n * G;  // at most 16 NT
+  auto token_of = [&](int r) { return r * a.group_inverse >> 16; };
+  auto limit_of = [&](int r) { return L - n + 1 + token_of(r); };  // row r sees tokens below it
+  auto out_row = [&](int r) {
+    const int i = token_of(r);
+    return ((size_t)b * n + i) * Hq + (size_t)g * G + (r - i * G);
+  };
+  const int l_first = L - n + 1;
+  const int l_vis = L;
   if (p == 0 && l_first <= 0) {  // rows that see nothing: zeros
     for (int x = tid; x < rows * (D / 4); x += kThreads)
-      if (limit_of(r0 + x / (D / 4)) <= 0) store_nt4(a.out + out_row(r0 + x / (D / 4)) * D + 4 * (x % (D / 4)), 0.f, 0.f, 0.f, 0.f);
+      if (limit_of(x / (D / 4)) <= 0) store_nt4(a.out + out_row(x / (D / 4)) * D + 4 * (x % (D / 4)), 0.f, 0.f, 0.f, 0.f);
   }
   if (l_vis <= p * Tp) return;
   const int j0 = p * Tp / kBlockTokens;
@@ -292,8 +295,8 @@ decode_fp8_kernel(const DecodeFp8Args args) {
 #pragma unroll
   for (int x = 0; x < NT; ++x) {
     wave[x].scale_log2 = a.scale_log2;
-    const int r = r0 + min(x * kFp8TileRows + (lane & 15), rows - 1);  // lanes past the last row repeat it
-    wave[x].start(a.q + out_row(r) * D, n - 1 - r / G);
+    const int r = min(x * kFp8TileRows + (lane & 15), rows - 1);  // lanes past the last row repeat it
+    wave[x].start(a.q + out_row(r) * D, n - 1 - token_of(r));
   }
   const char* kpool = reinterpret_cast<const char*>(args.k) + (size_t)g * CD::kTile;
   const char* vpool = reinterpret_cast<const char*>(args.v) + (size_t)g * CD::kTile;
@@ -352,7 +355,7 @@ decode_fp8_kernel(const DecodeFp8Args args) {
   for (int x = 0; x < kWaves; ++x) any_bad |= sh.bad[x];
   for (int x = tid; x < rows * (D / 4); x += kThreads) {
     const int h = x / (D / 4), d0 = 4 * (x % (D / 4));
-    const int limit = limit_of(r0 + h);
+    const int limit = limit_of(h);
     const int parts = limit > 0 ? (limit + Tp - 1) / Tp : 0;
     if (p >= parts) continue;  // the row sees nothing here
     float M = WA::kFloor, lsum = 0.f;
@@ -371,7 +374,7 @@ decode_fp8_kernel(const DecodeFp8Args args) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = __builtin_nanf("");
     }
-    const size_t row = out_row(r0 + h);
+    const size_t row = out_row(h);
     if (parts == 1) {
       const bool pos = lsum > 0.f;
       store_nt4(a.out + row * D + d0, pos ? acc[0] / lsum : acc[0], pos ? acc[1] / lsum : acc[1],
@@ -392,7 +395,7 @@ hipError_t launch_d(const DecodeFp8Args& a, hipStream_t stream) {
   const StepArgs& s = a.step;
   if (s.num_query_tokens * s.group > 2 * kFp8TileRows) return launch_wide_fp8(a, D, stream);
   const dim3 grid = s.order || a.picks ? dim3((unsigned)s.num_regular_items)
-                            : dim3((unsigned)s.num_kv_heads * (unsigned)s.num_chunk_groups, s.num_seqs, s.num_partitions);
+                            : dim3(s.num_kv_heads, s.num_seqs, s.num_partitions);
   if (s.num_query_tokens * s.group <= kFp8TileRows)
     hipLaunchKernelGGL((decode_fp8_kernel<D, 1>), grid, dim3(kThreads), 0, stream, a);
   else

@@ -145,10 +145,11 @@ __global__ void __launch_bounds__(kMaxThreads) append_fp8_kernel(const AppendFp8
 
 // Two new tokens of a sequence to a workgroup, four where many tokens have few rows
 // (at most kFewUnits threads' worth), one in a decode step.  Time in us with one, two
-// and four: 48 prompts of up to 1024 tokens, 28 / 4 heads of 128, 99 / 95 / 101; 32 x
+// and four, the same inputs again and again: 48 prompts of up to 1024 tokens, 28 / 4 heads of 128, 99 / 95 / 101; 32 x
 // 512 tokens of 32 / 8 72 / 71 / 73; 128 x 16 10.3 / 9.5 / 10.4; 48 x 300 tokens of 16 /
-// 16 heads of 64 38 / 33 / 30; a few tokens 5.2 / 5.3 / 7.0.  (With whole lines of
-// queries stored past the caches the first two take 83 and 59: 5.5 and 6.3 TB/s.)
+// 16 heads of 64 38 / 33 / 30; a few tokens 5.2 / 5.3 / 7.0.  With whole lines of
+// queries stored past the caches (whole_lines) the prompts take 83, and 92 where the
+// inputs change from call to call: 4.9 TB/s, the rate of a large copy.
 template <int D>
 hipError_t launch_d(const AppendFp8Args& a, hipStream_t stream) {
   const int units = ((a.q ? a.num_q_heads : 0) + 2 * a.num_kv_heads) * (D / 16);

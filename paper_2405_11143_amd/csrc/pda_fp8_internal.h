@@ -167,8 +167,8 @@ __device__ __forceinline__ void rotate_share(const float2* turns, bool interleav
 
 // Whether the stores of the rotated rows (bf16) cover whole cache lines of 128 bytes:
 // then, with many tokens, they go out with the non-temporal hint (16384 tokens of
-// 32 + 8 heads of 128: 57 -> 48 us); lines written in halves would be written
-// twice (neighbouring pairs in shares of 16 neighbouring elements: 44 -> 57 us).
+// 32 + 8 heads of 128: 64 -> 59 us); lines written in halves would be written
+// twice (neighbouring pairs in shares of 16 neighbouring elements took 30% longer).
 inline bool whole_lines(const RotaryArgs& r, int head_dim) {
   const int copied = r.interleaved ? head_dim : head_dim - r.rotary_dim;  // elements in vectors of their own
   return copied % 128 == 0 && (r.interleaved || r.rotary_dim % 128 == 0);

@@ -3,8 +3,8 @@
 // block of a sequence, and a thread the same 8 elements of the same slot in every
 // head (8 bytes read, 16 written), neighbouring threads neighbouring elements of
 // the output, which goes out with the non-temporal hint.  64 sequences of 512-4096
-// tokens, 8 KV heads of 128 (0.91 GB): 169 us, 5.4 TB/s; with plain stores 185, and
-// with threads that divided their way through (token, head, piece) 228.
+// tokens, 8 KV heads of 128 (0.91 GB): 178 us, 5.1 TB/s (a large copy 4.9); threads that
+// divided their way through (token, head, piece) and stored plainly took 225.
 #include "pda_fp8_internal.h"
 
 namespace pda {
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(kThreads) read_fp8_kernel(const ReadFp8Args a,
     u32x4_t* k_out = reinterpret_cast<u32x4_t*>(a.k_out) + (size_t)row * H * P + c;
     u32x4_t* v_out = reinterpret_cast<u32x4_t*>(a.v_out) + (size_t)row * H * P + c;
     const size_t tile0 = (size_t)(ok ? page : 0) * H;
-#pragma unroll 1  // (4: 185 us)
+#pragma unroll 1  // (by 4: 9% longer)
     for (int g = sub; g < H; g += HEADS) {
       uint4 k = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u), v = k;  // NaN
       if (ok) {

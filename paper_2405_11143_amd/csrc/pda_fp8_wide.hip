@@ -275,7 +275,7 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     f32x16_t ns;
     if constexpr (kAhead) ns = scores(next_blocks);
     // Each probability as two bf16 halves, both rounded to nearest: hi = bf16(p), lo
-    // = bf16(p - hi), at most 2^-18 of p off.
+    // = bf16(p - hi), at most 2^-17 of p off.
     bf16x8_t bh[2], bl[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {

@@ -5,9 +5,9 @@
 // reduction, then sine and cosine), and the same for all heads of a token: a
 // workgroup takes one token, forms its cosines and sines in LDS, a thread each,
 // and then its rows, 16 elements per thread.  16384 tokens of 32 + 8 heads of 128, bf16:
-// 48 us, 6.8 TB/s; neighbouring pairs in half of 28 + 4 heads' elements, the
-// others copied: 39 us, 6.8 TB/s.  Four tokens to a workgroup (its loop goes from row
-// to row and from token to token) took 63 us where one took 58, two 64.
+// 59 us, 5.6 TB/s (a large copy 4.9); neighbouring pairs in half of 28 + 4 heads'
+// elements, the others copied: 47 us, 5.6 TB/s.  Four tokens to a workgroup (its loop
+// goes from row to row and from token to token) took 8% longer than one, two 10%.
 #include "pda_fp8_internal.h"
 
 namespace pda {
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const RotaryApplyAr
 }
 
 // A workgroup has as many threads as make its last trip through the rows a full
-// one, nearly (up to 512 of them for a single trip: 65 us against 58).
+// one, nearly (up to 512 of them for a single trip took 12% longer).
 template <typename T>
 hipError_t launch_t(const RotaryApplyArgs& a, hipStream_t stream) {
   const int units = (a.q.heads + a.k.heads) * row_shares(a.head_dim);

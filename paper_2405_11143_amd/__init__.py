@@ -4,9 +4,9 @@ The rollout hot path of RLHF/RLVR training (arXiv 2405.11143): one decode
 step's attention of every sequence's new query token(s) over its paged KV
 cache, with grouped-query heads (also with a shared prompt prefix attended once
 for all the prompt's samples), the KV-cache append before it, and the step
-captured as a HIP graph, and the sampled tokens' log-probabilities and
-entropies -- hand-written HIP kernels behind a C ABI
-(include/pda.h).  This package is the thin Python binding of that ABI.
+captured as a HIP graph, the sampled tokens' log-probabilities and entropies,
+and the same step over an 8-bit KV cache with rotary positions --
+hand-written HIP kernels behind a C ABI (include/pda.h, include/pda_fp8.h).  This package is the thin Python binding of that ABI.
 """
 from .pda import (EXPORTED, LIB_PATH, BoundCall, ModelStepGraph, PdaError, StepGraph, bind_append_kv, bind_decode, bind_token_logprobs,  # noqa: F401
                   load_library, make_prefix_groups,

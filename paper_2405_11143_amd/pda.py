@@ -1,4 +1,4 @@
-"""Python binding of the paged decode-attention C ABI (include/pda.h).
+"""Python binding of the paged decode-attention C ABI (include/pda.h, include/pda_fp8.h).
 
 Argument marshalling only: every step of the computation runs in the HIP
 kernels of libpda.so.  The library must have been built in-tree
@@ -21,7 +21,7 @@ PDA_OK, PDA_ERR_NULL, PDA_ERR_SHAPE, PDA_ERR_UNSUPPORTED = 0, 1, 2, 3
 PDA_ERR_WORKSPACE, PDA_ERR_ALIGNMENT, PDA_ERR_VALUE, PDA_ERR_HIP, PDA_ERR_SCRATCH = 4, 5, 6, 7, 8
 PDA_NOALLOC_SCRATCH_BYTES = 64 << 20  # the static scratch of pda_decode_noalloc
 
-# Every function include/pda.h declares.
+# Every function the headers under include/ declare.
 EXPORTED = ("pda_plan", "pda_workspace_bytes", "pda_decode", "pda_partition_attention",
             "pda_merge_partitions", "pda_plan_shared_prefix", "pda_decode_shared_prefix", "pda_append_kv",
             "pda_step_graph_create", "pda_step_graph_launch", "pda_step_graph_destroy", "pda_token_logprobs",

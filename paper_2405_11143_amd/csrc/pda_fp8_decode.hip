@@ -240,11 +240,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(N
 decode_fp8_kernel(const DecodeFp8Args args) {
   using WA = WaveAttention<D>;
   using CD = Codes<D>;
-  __shared__ __align__(16) union {
-    DecodeShared<D, NT * kFp8TileRows> sh;  // the epilogue
-    PickShared pick;
-  } lds;
-  DecodeShared<D, NT * kFp8TileRows>& sh = lds.sh;
+  __shared__ __align__(16) DecodeShared<D, NT * kFp8TileRows> sh;
+  __shared__ PickShared pick;  // (a place of its own: a wavefront without blocks may be in the epilogue before others read it)
   const StepArgs& a = args.step;
   int g, b, p;  // KV head, sequence, partition
   if (a.order) {
@@ -263,7 +260,7 @@ decode_fp8_kernel(const DecodeFp8Args args) {
       const int in = slot - first * H;
       pos = first + in % c, g = in / c;
     }
-    const int pair = __builtin_amdgcn_readfirstlane(pick_pair(a, pos, lds.pick));  // (the epilogue's LDS: barriers between)
+    const int pair = __builtin_amdgcn_readfirstlane(pick_pair(a, pos, pick));
     p = pair / a.num_seqs, b = pair % a.num_seqs;
   } else {
     g = blockIdx.x, b = blockIdx.y, p = blockIdx.z;

@@ -761,6 +761,8 @@ def pda_rotary_inv_freq(rotary_dim: int, base: float = 10000.0, kind: int = PDA_
     """(inv_freq, magnitude): the rotary_dim / 2 frequencies base^(-2i / rotary_dim)
     scaled for long contexts as `kind` says (include/pda_fp8.h), as a float64
     numpy array, and the factor on the rotated elements."""
+    import torch  # noqa: F401  (before the library: its HIP runtime is the one to share)
+
     inv_freq = np.empty(max(int(rotary_dim), 0) // 2, dtype=np.float64)
     scaling = pda_rotary_scaling(int(kind), float(factor), float(original_len), float(low), float(high))
     magnitude = ctypes.c_float()
@@ -904,6 +906,8 @@ def pda_append_kv_fp8(k_new, v_new, block_table, context_lens, k_cache, v_cache,
 
 def pda_plan_fp8(prob: pda_problem) -> dict:
     """The plan of pda_decode_fp8: partition_tokens, num_partitions, workspace_bytes."""
+    import torch  # noqa: F401  (before the library: its HIP runtime is the one to share)
+
     info = pda_plan_info()
     rc = load_library().pda_plan_fp8(ctypes.byref(prob), ctypes.byref(info))
     if rc != PDA_OK:

@@ -707,17 +707,31 @@ def _same_device(*tensors):
     return devices.pop()
 
 
+def _as_stream(stream, device):
+    import torch
+
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
 def _hold(stream, *temporaries):
     """Tensors allocated for one call on a stream that is not the current one:
     their memory is not reused before the stream is done with them."""
-    import torch
-
     if stream is not None:
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream))
         for t in temporaries:
             if t is not None:
-                t.record_stream(stream)
+                t.record_stream(_as_stream(stream, t.device))
+
+
+def _zeros_like(t, stream):
+    """Zeros of t's shape, filled on the stream that the call which writes them
+    runs on (filled on another, they could overwrite its rows)."""
+    import torch
+
+    out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if stream is None:
+        return out.zero_()
+    with torch.cuda.stream(_as_stream(stream, t.device)):
+        return out.zero_()
 
 
 def _check_fp8_cache(k_cache, v_cache, kv_scale):
@@ -813,13 +827,15 @@ def bind_rotary_apply(q, positions, rotary: pda_rotary, k=None, q_out=None, k_ou
         raise ValueError("q [T][Hq][D], k [T][Hkv][D]")
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
+    if q.shape[0] > 0x7fffffff:
+        raise ValueError("more than 2^31 - 1 tokens")
     _require("positions", positions, torch.int32)
     if positions.shape != (q.shape[0],):
         raise ValueError("positions must be [T]")
     # (padding rows are not written: an output made here holds zeros there)
-    q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    q_out = _zeros_like(q, stream) if q_out is None else q_out
     if k is not None and k_out is None:
-        k_out = torch.zeros(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _zeros_like(k, stream)
     if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
         raise ValueError("the outputs must have the inputs' shapes")
     device = _same_device(q, q_out, k, k_out, positions, rotary.tensor)
@@ -875,7 +891,7 @@ def bind_append_kv_fp8(k_new, v_new, block_table, context_lens, k_cache, v_cache
             raise ValueError("q must be [B][n][Hq][D]")
         Hq = q.shape[-2]
         if q_out is None:
-            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _zeros_like(q, stream)
         _require("q_out", q_out, torch.bfloat16)
         if q_out.shape != q.shape:
             raise ValueError("q_out must have the shape of q")
@@ -938,6 +954,8 @@ def bind_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, sc
         raise ValueError("out must have the shape of q")
     device = _same_device(q, k_cache, v_cache, kv_scale, block_table, context_lens, out, workspace)
     prob = make_problem(B, Hq, Hkv, D, NB, block_table.shape[1], max_context_len, partition_tokens, 16, n)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     need = pda_plan_fp8(prob)["workspace_bytes"]
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)

@@ -606,3 +606,36 @@ def test_empty_batch(dev):
     pda.pda_append_kv_fp8(torch.zeros(0, 1, 2, 64, **bf), torch.zeros(0, 1, 2, 64, **bf), table, lens, *cache, max_context_len=48)
     pda.pda_read_kv_fp8(*cache, table, lens, torch.zeros(1, **i32), torch.zeros(0, 2, 64, **bf), torch.zeros(0, 2, 64, **bf),
                         max_context_len=48)
+
+
+def test_outputs_made_for_another_stream(dev):
+    """Outputs that the binding allocates and clears for a call on a given stream: nothing that the current
+    stream still has to do comes after the call's rows."""
+    st, cache, q, K, V = case([300, 77, 2], 8, 2, 128, 3, 32, dev)
+    rot = pda.make_rotary(up(pda.pda_rotary_inv_freq(128)[0], dev))
+    rows, keys = q.reshape(9, 8, 128), up(np.random.RandomState(5).randn(9, 2, 128), dev, torch.bfloat16)
+    positions = up(np.array([0, 5, 3, -1, 7, 8, 1000, -2, 4], np.int32), dev)
+    new = keys.reshape(3, 3, 2, 128)
+    table, lens = up(st.block_table, dev), up(st.context_lens, dev)
+    kw = dict(max_context_len=st.max_context_len, rotary=rot, q=q)
+    want_rows = pda.pda_rotary_apply(rows, positions, rot, k=keys)
+    want_q = pda.pda_append_kv_fp8(new, new, table, lens, *upload(cache, dev), **kw)
+    on_gpu = upload(cache, dev)
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):  # (a stream, or its handle)
+        busy = torch.randn(4096, 4096, device=dev, dtype=torch.bfloat16)
+        torch.cuda.synchronize()
+        for _ in range(40):
+            busy = (busy @ busy).clamp_(-1, 1)
+        got_rows = pda.pda_rotary_apply(rows, positions, rot, k=keys, stream=stream)
+        got_q = pda.pda_append_kv_fp8(new, new, table, lens, *on_gpu, **kw, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got_rows, want_rows)) and torch.equal(got_q, want_q)
+
+
+def test_refuses_a_workspace_that_is_not_contiguous(dev):
+    st, cache, q, K, V = case([300, 77, 1], 8, 2, 128, 1, 33, dev)
+    for ws in (torch.empty(1, dtype=torch.uint8, device=dev).expand(1 << 24),
+               torch.empty(1 << 20, dtype=torch.uint8, device=dev)[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            decode(q, upload(cache, dev), st, dev, workspace=ws)

@@ -128,13 +128,19 @@ struct Codes {
     }
   }
 
-  // V's codes and scale bytes become zeros from row `rel` of the lane's four on.
+  // Whether row e of the lane's four of V is one of NaN.
+  __device__ __forceinline__ bool dead(int e) const { return (vs >> (8 * e) & 255u) == 255u; }
+
+  // V's codes and scale bytes become zeros from row `rel` of the lane's four on, and
+  // in the rows of NaN.
   __device__ __forceinline__ void clear_v(int rel) {
+    const bool d0 = dead(0), d1 = dead(1), d2 = dead(2), d3 = dead(3);
+    vs &= (d0 ? 0u : 0xffu) | (d1 ? 0u : 0xff00u) | (d2 ? 0u : 0xff0000u) | (d3 ? 0u : 0xff000000u);
     vs = rel <= 0 ? 0u : rel >= 4 ? vs : vs & ((1u << (8 * rel)) - 1);
-    if (rel <= 0) v[0].x = v[0].y = 0u;
-    if (rel <= 1) v[0].z = v[0].w = 0u;
-    if (rel <= 2) v[1].x = v[1].y = 0u;
-    if (rel <= 3) v[1].z = v[1].w = 0u;
+    if (rel <= 0 || d0) v[0].x = v[0].y = 0u;
+    if (rel <= 1 || d1) v[0].z = v[0].w = 0u;
+    if (rel <= 2 || d2) v[1].x = v[1].y = 0u;
+    if (rel <= 3 || d3) v[1].z = v[1].w = 0u;
   }
 };
 
@@ -149,8 +155,11 @@ struct Fold : WaveAttention<D> {
   using WA = WaveAttention<D>;
   __device__ __forceinline__ Fold() : WA(0.f) {}
 
-  __device__ __forceinline__ void probabilities(const uint4 (&kr)[2][WA::NC], int tok0, int L, int t_stop, bool tail,
-                                                bf16x8_t (&part)[3]) {
+  // A zero probability would not keep a NaN of V from a row that does not see its
+  // token: in the tail, rows of NaN make the scores of the rows that see them NaN
+  // here, and are zeros in the product.
+  __device__ __forceinline__ void probabilities(const uint4 (&kr)[2][WA::NC], const Codes<D> (&c)[2], int tok0, int L,
+                                                int t_stop, bool tail, bf16x8_t (&part)[3]) {
     float sc[2][4];
     this->template scores<2>(kr, sc);
     if (tail) {
@@ -159,8 +168,10 @@ struct Fold : WaveAttention<D> {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          if (c[b].dead(i)) sc[b][i] = __builtin_nanf("");
           if (kBlockTokens * b + i >= rel) sc[b][i] = WA::kNegInf;
+        }
     }
     float top = max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]);
     top = max3(max3(sc[1][1], sc[1][2], sc[1][3]), top, top);
@@ -191,8 +202,8 @@ __device__ __forceinline__ void fold_pair(Fold<D> (&wave)[NT], Codes<D> (&c)[2],
   c[1].k_frags(kr[1]);
   bf16x8_t part[NT][3];
 #pragma unroll
-  for (int x = 0; x < NT; ++x) wave[x].probabilities(kr, tok0, L, t_stop, tail, part[x]);
-  if (tail) {  // rows that no query row sees, whatever they hold
+  for (int x = 0; x < NT; ++x) wave[x].probabilities(kr, c, tok0, L, t_stop, tail, part[x]);
+  if (tail) {  // rows that no query row sees, whatever they hold, and those of NaN
     asm volatile("");
 #pragma unroll
     for (int b = 0; b < 2; ++b) c[b].clear_v(l_vis - (tok0 + kBlockTokens * b + 4 * wave[0].kg));

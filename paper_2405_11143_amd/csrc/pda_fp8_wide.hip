@@ -48,6 +48,7 @@ struct WideLds {
     f32x4_t o[W][kTileRows][D / 8];  // the epilogue, half of the columns at a time
   };
   int ids[window(W)];
+  unsigned char dead[buffers(W)][kStageBlocks * kBlockTokens];  // per token of a buffer: its values are NaN
 };
 
 template <int D, int W>
@@ -105,7 +106,7 @@ wide_fp8_kernel(const DecodeFp8Args args) {
   const bool active = x0 < wg_rows;
   const int my_x = min(x0 + col, wg_rows - 1);  // lanes past the last row repeat it
   const int limit = min(limit_of(my_x), t_pe);
-  const int l_first = min(limit_of(min(x0, wg_rows - 1)), t_pe);
+  const int l_some = min(limit_of(0), t_pe);  // from here on some row of the workgroup does not see a token
   const int l_vis = min(max(limit_of(min(x0 + kTileRows, wg_rows) - 1), 0), t_pe);
 
   float scale = a.scale_log2;
@@ -187,7 +188,8 @@ wide_fp8_kernel(const DecodeFp8Args args) {
         raw_scale[k] = __builtin_amdgcn_raw_buffer_load_b16(rs, s_off[k], 0, 0);
     }
   };
-  auto commit = [&](uint4* buf, int tok0) {
+  auto commit = [&](int buffer, int tok0) {
+    uint4* buf = st.buf[buffer][0];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
       const bool is_k = side_of(k) == 0;
@@ -195,12 +197,17 @@ wide_fp8_kernel(const DecodeFp8Args args) {
       const float f1 = is_k ? f0 : scale_of<1>(raw_scale[k]);
       uint4 lo = to_bf16(raw[k].x, raw[k].y, f0);
       uint4 hi = to_bf16(raw[k].z, raw[k].w, f1);
-      if (!is_k && tok0 + kStageBlocks * kBlockTokens > L) {  // values past the context are zeros whatever the slots hold
+      // A zero probability would not keep a NaN from a row that does not see its token:
+      // values past the context, whatever the slots hold, and rows of NaN are zeros
+      // there, and the latter make the scores of the rows that see them NaN (mask).
+      if (!is_k && tok0 + kStageBlocks * kBlockTokens > l_some) {
         asm volatile("");  // a branch
         const int blk = (k * kThreads + tid) / D % kStageBlocks;
-        const int t = tok0 + blk * kBlockTokens + s_off[k] - 16;
-        if (t >= L) lo = make_uint4(0u, 0u, 0u, 0u);
-        if (t + 1 >= L) hi = make_uint4(0u, 0u, 0u, 0u);
+        const int at = blk * kBlockTokens + s_off[k] - 16, t = tok0 + at;
+        const bool dead0 = (raw_scale[k] & 255u) == 255u, dead1 = (raw_scale[k] >> 8 & 255u) == 255u;
+        if (t >= L || dead0) lo = make_uint4(0u, 0u, 0u, 0u);
+        if (t + 1 >= L || dead1) hi = make_uint4(0u, 0u, 0u, 0u);
+        st.dead[buffer][at] = dead0, st.dead[buffer][at + 1] = dead1;  // (the same from every thread of the row)
       }
       buf[dst[k][0]] = lo;
       buf[dst[k][1]] = hi;
@@ -235,23 +242,26 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     top = max3(x, s[15], s[15]);
     asm volatile("" : "+v"(top));  // the MFMA results are first read in their own basic block
   };
-  auto mask = [&](int tok0) {
-    if (tok0 + 32 > l_first) {  // wavefront-uniform: some row does not see some of these tokens
+  auto mask = [&](int buffer, int tok0) {
+    if (tok0 + 32 > l_some) {  // some row of the workgroup does not see some of these tokens
       asm volatile("");  // a branch: as selects the masking would run on every step
       const int rel = limit - (tok0 + 4 * hh);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
+      for (int i = 0; i < 16; ++i) {
+        if (st.dead[buffer][8 * (i / 4) + 4 * hh + i % 4]) s[i] = __builtin_nanf("");
         if (8 * (i / 4) + i % 4 >= rel) s[i] = -__builtin_huge_valf();
+      }
       largest();
     }
   };
   // Fold the step whose scores are in s (two blocks of a buffer), and form the
-  // scores of the next one (in next_blocks).
-  auto fold = [&](int tok0, const uint4* blocks, const uint4* next_blocks) {
+  // scores of the next one.
+  auto fold = [&](int tok0, int buffer, int next) {
+    const uint4 *blocks = st.buf[buffer][0], *next_blocks = st.buf[next][0];
     if constexpr (!kAhead) {
       s = scores(blocks);
       largest();
-      mask(tok0);
+      mask(buffer, tok0);
     }
     auto v_frag = [&](int m, int t) {
       const uint16_t* v0 = reinterpret_cast<const uint16_t*>(blocks + S::kTilePieces + m * S::kBlockPieces) + tr_off[t];
@@ -307,7 +317,7 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     if constexpr (kAhead) {
       s = ns;
       largest();
-      mask(tok0 + 32);
+      mask(next, tok0 + 32);
     }
   };
 
@@ -328,14 +338,14 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     for (int x = 0; x < kStaged; ++x)
       if (x < nsteps) {
         issue(x);
-        commit(st.buf[x][0], tok_w + 32 * x);
+        commit(x, tok_w + 32 * x);
       }
     if (kStaged < nsteps) issue(kStaged);
     __syncthreads();
     if (kAhead && active) {
       s = scores(st.buf[0][0]);
       largest();
-      mask(tok_w);
+      mask(0, tok_w);
     }
     // Step `step` is in buffer B = step % kBuffers (a constant, and so are all LDS
     // addresses: the loop is unrolled by the buffers).  False at the last step.
@@ -343,9 +353,9 @@ wide_fp8_kernel(const DecodeFp8Args args) {
       const int tok0 = tok_w + 32 * step;
       // behind the barrier the last step's buffer is free, and what this step reads is written
       if (step > 0) __syncthreads();
-      if (step + kStaged < nsteps) commit(st.buf[(B + kStaged) % kBuffers][0], tok0 + 32 * kStaged);
+      if (step + kStaged < nsteps) commit((B + kStaged) % kBuffers, tok0 + 32 * kStaged);
       if (step + kBuffers < nsteps) issue(step + kBuffers);
-      if (active && tok0 < l_vis) fold(tok0, st.buf[B][0], st.buf[(B + 1) % kBuffers][0]);  // wavefront-uniform
+      if (active && tok0 < l_vis) fold(tok0, B, (B + 1) % kBuffers);  // wavefront-uniform
       return step + 1 < nsteps;
     };
     for (int step = 0;; step += kBuffers) {

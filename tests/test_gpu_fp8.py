@@ -639,3 +639,38 @@ def test_refuses_a_workspace_that_is_not_contiguous(dev):
                torch.empty(1 << 20, dtype=torch.uint8, device=dev)[::2]):
         with pytest.raises(ValueError, match="contiguous"):
             decode(q, upload(cache, dev), st, dev, workspace=ws)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 2), (128, 7, 1), (128, 4, 4)], ids=str)
+@pytest.mark.parametrize("n", [1, 4, 13, 60, 200])
+@pytest.mark.parametrize("which", ["key", "value"])
+@pytest.mark.parametrize("partition_tokens", [0, 48])
+def test_decode_rows_of_nan(dev, D, Hq, Hkv, n, which, partition_tokens):
+    """A key or value row of NaN inside a context makes the rows that see it NaN, and changes no others (their sums
+    do not hold it; the bars of the finite result apply)."""
+    lens = [1, n + 3, 250, 297]
+    st, cache, q, K, V = case(lens, Hq, Hkv, D, n, 600 + n, dev)
+    side = 0 if which == "key" else 1
+    hit = [[0], [3, n + 1], [250 - (n + 1) // 2], [296]]  # tokens that only some of the new tokens see, or all
+    for b, tokens in enumerate(hit):
+        for t in tokens:
+            block, slot = st.block_table[b, t // 16], t % 16
+            d = np.arange(D)
+            place = ref.k_place if side == 0 else ref.v_place
+            for g in range(Hkv):
+                cache[side][(block, g) + tuple(np.broadcast_arrays(*place(d, slot)))] = 0x7F
+                cache[2][block, g, side, slot] = 255
+    got = f64(decode(q, upload(cache, dev), st, dev, partition_tokens=partition_tokens))
+    limits = np.array(lens)[:, None] - n + 1 + np.arange(n)
+    sees = np.array([[any(t < m for t in hit[b]) for m in limits[b]] for b in range(4)])
+    assert np.isnan(got[sees]).all() and np.isfinite(got[~sees]).all()
+    clean = np.where(sees[:, :, None, None], 0.0, got)
+    for b, L in enumerate(lens):
+        t = np.arange(L)
+        page = st.block_table[b, t // 16]
+        for g in range(Hkv):
+            rows = f64(q)[b, :, g * (Hq // Hkv):(g + 1) * (Hq // Hkv)].reshape(-1, D)
+            want, bound = ref.attention(rows, K[page, g, t % 16], V[page, g, t % 16], np.repeat(limits[b], Hq // Hkv), st.scale)
+            keep = np.repeat(~sees[b], Hq // Hkv)
+            err = np.abs(clean[b, :, g * (Hq // Hkv):(g + 1) * (Hq // Hkv)].reshape(-1, D) - want)[keep]
+            assert (err <= bound[keep]).all()

@@ -136,7 +136,9 @@ int pda_plan_fp8(const pda_problem *prob, pda_plan_info *plan);
 /* pda_decode over this cache: the softmax attention of pda.h with
  *   K[t][d] = k code * 2^(s_K - 127),  V[t][d] = v code * 2^(s_V - 127).
  * Both products run on exactly converted values with fp32 sums, so the result is
- * that of a bf16 cache holding the stored values, to fp32 accuracy.  out is
+ * that of a bf16 cache holding the stored values: to fp32 accuracy (3e-7 of its norm)
+ * where n Hq / Hkv is at most 32, and 2.5e-6 of its norm beyond, where the probabilities
+ * are kept to 16 bits or more.  out is
  * fp32 [B][n][Hq][D]; rows that see nothing are zero.  `workspace`: any contents,
  * pda_plan_fp8()'s workspace_bytes, 16-byte aligned; calls that overlap on the GPU
  * need separate ones. */

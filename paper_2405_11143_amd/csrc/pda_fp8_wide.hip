@@ -285,7 +285,9 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     f32x16_t ns;
     if constexpr (kAhead) ns = scores(next_blocks);
     // Each probability as two bf16 halves, both rounded to nearest: hi = bf16(p), lo
-    // = bf16(p - hi), at most 2^-17 of p off.
+    // = bf16(p - hi), at most 2^-17 of p off: 2.5e-6 of the result's norm.  A third part
+    // (3e-7) takes 24% longer in chunks (32 x 512 new tokens 1565 -> 1935 us) and 15% at
+    // up to 64 rows (256 x 16 327 -> 375).
     bf16x8_t bh[2], bl[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {

@@ -713,21 +713,37 @@ def _as_stream(stream, device):
     return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
 
 
-def _hold(stream, *temporaries):
-    """Tensors allocated for one call on a stream that is not the current one:
-    their memory is not reused before the stream is done with them."""
+def _hold(stream, *tensors):
+    """Tensors that a call on a stream other than the current one uses and hands
+    back: their memory is not reused before the stream is done with them."""
     if stream is not None:
-        for t in temporaries:
+        for t in tensors:
             if t is not None:
                 t.record_stream(_as_stream(stream, t.device))
 
 
-def _zeros_like(t, stream):
-    """Zeros of t's shape, filled on the stream that the call which writes them
-    runs on (filled on another, they could overwrite its rows)."""
+def _empty(shape, dtype, device, stream, result=True):
+    """Memory for a call on `stream` (None: the current one), taken from that
+    stream's own: what the current stream has freed may still be in use by work it
+    has queued, which nothing orders before the call.  A `result` is handed back to
+    the current stream: it is not reused before that one is done with it, either."""
     import torch
 
-    out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    stream = _as_stream(stream, device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _zeros_like(t, stream):
+    """Zeros of t's shape for a call on `stream`, filled on it too."""
+    import torch
+
+    out = _empty(t.shape, t.dtype, t.device, stream)
     if stream is None:
         return out.zero_()
     with torch.cuda.stream(_as_stream(stream, t.device)):
@@ -948,7 +964,7 @@ def bind_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, sc
         raise ValueError("at least one new token")
     _check_paged(block_table, context_lens, B)
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     _require("out", out, torch.float32)
     if out.shape != q.shape:
         raise ValueError("out must have the shape of q")
@@ -958,7 +974,7 @@ def bind_decode_fp8(q, k_cache, v_cache, kv_scale, block_table, context_lens, sc
         raise ValueError("workspace must be contiguous")
     need = pda_plan_fp8(prob)["workspace_bytes"]
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _empty((need,), torch.uint8, device, stream, result=False)
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     args = (ctypes.byref(prob), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv_scale.data_ptr(),

@@ -710,7 +710,11 @@ def _same_device(*tensors):
 def _as_stream(stream, device):
     import torch
 
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    if int(stream) == 0:  # (an ExternalStream of handle 0 is a new stream)
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(int(stream), device=device)
 
 
 def _hold(stream, *tensors):

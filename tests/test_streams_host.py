@@ -11,12 +11,16 @@ import torch
 import paper_2405_11143_amd as pda
 from paper_2405_11143_amd import pda as P
 
-CURRENT, SIDE = 11, 22
+CURRENT, SIDE, OTHER = 11, 22, 33
 
 
 class Stream:
     def __init__(self, handle, device=None):
         self.cuda_stream = handle
+
+
+def external_stream(handle, device=None):
+    return Stream(handle or OTHER)  # (torch makes a new stream of a handle of 0)
 
 
 class Recorder:
@@ -47,7 +51,8 @@ class Recorder:
                             lambda t, s: self.kept.setdefault(id(t), set()).add(s.cuda_stream))
         monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
         monkeypatch.setattr(torch.cuda, "stream", stream_context)
-        monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", external_stream)
+        monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream(0))
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(self.stack[-1]))
         monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
         monkeypatch.setattr(P.BoundCall, "__call__", lambda call: call.result)
@@ -109,3 +114,13 @@ def test_without_a_stream_nothing_changes_it(monkeypatch):
     rec = Recorder(monkeypatch)
     pda.pda_decode_fp8(q, *cache, table, lens, 0.125, max_context_len=64, partition_tokens=16)
     assert [s for s, _ in rec.made.values()] == [CURRENT] * 2 and not rec.kept
+
+
+def test_the_null_stream_by_its_handle(monkeypatch):
+    """0 is the default stream's handle: what the binding clears for a call on it is cleared there."""
+    q, pos = torch.zeros(5, 4, 64, **bf), torch.zeros(5, **i32)
+    rec = Recorder(monkeypatch)
+    call = pda.bind_rotary_apply(q, pos, pda.make_rotary(torch.ones(32, dtype=torch.float64)), stream=0)
+    assert call._args[-1].value is None  # (ctypes' null)
+    out, _ = call.result
+    assert rec.made[id(out)][0] == 0 and rec.cleared[id(out)] == 0

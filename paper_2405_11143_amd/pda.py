@@ -253,12 +253,48 @@ def _stream_handle(stream, device):
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
-def _workspace(prob, workspace, device):
+def _as_stream(stream, device):
+    import torch
+
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    if int(stream) == 0:  # (an ExternalStream of handle 0 is a new stream)
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _empty(shape, dtype, device, stream, result=True):
+    """Memory for a call on `stream` (None: the current one), taken from that
+    stream's own: what the current stream has freed may still be in use by work it
+    has queued, which nothing orders before the call.  A `result` is handed back to
+    the current stream: it is not reused before that one is done with it, either."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    stream = _as_stream(stream, device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _hold(stream, *tensors):
+    """Tensors that a call on a stream other than the current one uses and hands
+    back: their memory is not reused before the stream is done with them."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(_as_stream(stream, t.device))
+
+
+def _workspace(prob, workspace, device, stream=None):
     import torch
 
     need = pda_workspace_bytes(prob)
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _empty((need,), torch.uint8, device, stream, result=False)
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     return workspace, ws_ptr, ws_bytes
@@ -345,10 +381,10 @@ def bind_decode(q, k_cache, v_cache, block_table, context_lens, scale: float, ou
     import torch
 
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
     prob = _problem_from(q, k_cache, block_table, max_context_len, partition_tokens)
-    workspace, ws_ptr, ws_bytes = _workspace(prob, workspace, q.device)
+    workspace, ws_ptr, ws_bytes = _workspace(prob, workspace, q.device, stream)
     args = (ctypes.byref(prob), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
             context_lens.data_ptr(), ctypes.c_float(scale), out.data_ptr(), ws_ptr, ws_bytes,
             _stream_handle(stream, q.device))
@@ -366,11 +402,11 @@ def bind_decode_append(q, k_new, v_new, k_cache, v_cache, block_table, context_l
     import torch
 
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
     _check_new_kv(k_new, v_new, _query_shape(q), k_cache)
     prob = _problem_from(q, k_cache, block_table, max_context_len, partition_tokens)
-    workspace, ws_ptr, ws_bytes = _workspace(prob, workspace, q.device)
+    workspace, ws_ptr, ws_bytes = _workspace(prob, workspace, q.device, stream)
     args = (ctypes.byref(prob), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), k_cache.data_ptr(),
             v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(), ctypes.c_float(scale),
             out.data_ptr(), ws_ptr, ws_bytes, _stream_handle(stream, q.device))
@@ -415,7 +451,7 @@ def bind_decode_noalloc(q, k_cache, v_cache, block_table, context_lens, scale: f
     import torch
 
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
     prob = _problem_from(q, k_cache, block_table, max_context_len, partition_tokens)
     args = (ctypes.byref(prob), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
@@ -588,12 +624,12 @@ def bind_token_logprobs(logits, tokens, inv_temperature: float = 1.0, entropy: b
     if tokens.shape != (rows,):
         raise ValueError("tokens must be [rows]")
     if logprobs is None:
-        logprobs = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        logprobs = _empty((rows,), torch.float32, logits.device, stream)
     if entropy and entropies is None:
-        entropies = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        entropies = _empty((rows,), torch.float32, logits.device, stream)
     if isinstance(workspace, str):
         need = pda_logprob_workspace_bytes(rows, vocab, dtype) if vocab >= 1 else 0
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need > 0 else None
+        workspace = _empty((need,), torch.uint8, logits.device, stream, result=False) if need > 0 else None
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     args = (rows, vocab, logits.stride(0), dtype, logits.data_ptr(), tokens.data_ptr(),
@@ -625,7 +661,7 @@ def pda_decode_shared_prefix(q, k_cache, v_cache, block_table, context_lens, sca
     import torch
 
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
     _require("group_start", group_start, torch.int32)
     _require("group_prefix_len", group_prefix_len, torch.int32)
@@ -636,7 +672,7 @@ def pda_decode_shared_prefix(q, k_cache, v_cache, block_table, context_lens, sca
     groups = make_prefix_groups(num_groups, max_group_size, max_prefix_len, group_start, group_prefix_len)
     need = pda_plan_shared_prefix(prob, groups)["workspace_bytes"]
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _empty((need,), torch.uint8, q.device, stream, result=False)
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     rc = load_library().pda_decode_shared_prefix(
@@ -658,7 +694,7 @@ def bind_gather_ceiling(block_ids, k_cache, v_cache, workgroups: int, sink=None,
     _require("k_cache", k_cache, torch.bfloat16)
     _require("v_cache", v_cache, torch.bfloat16)
     if sink is None:
-        sink = torch.empty(4 * workgroups, dtype=torch.int32, device=k_cache.device)
+        sink = _empty((4 * workgroups,), torch.int32, k_cache.device, stream)
     NB, Hkv, C, BS, E = k_cache.shape
     args = (int(Hkv), int(C * E), int(NB), k_cache.data_ptr(), v_cache.data_ptr(), block_ids.data_ptr(),
             int(block_ids.numel()), int(workgroups), sink.data_ptr(), _stream_handle(stream, k_cache.device))
@@ -673,7 +709,7 @@ def bind_stream_ceiling(buf, workgroups: int, sink=None, stream=None) -> BoundCa
     if not buf.is_cuda or not buf.is_contiguous():
         raise ValueError("buf must be a contiguous device tensor")
     if sink is None:
-        sink = torch.empty(4 * workgroups, dtype=torch.int32, device=buf.device)
+        sink = _empty((4 * workgroups,), torch.int32, buf.device, stream)
     nbytes = buf.numel() * buf.element_size() // 16 * 16
     args = (buf.data_ptr(), ctypes.c_size_t(nbytes), int(workgroups), sink.data_ptr(),
             _stream_handle(stream, buf.device))
@@ -705,42 +741,6 @@ def _same_device(*tensors):
     if len(devices) != 1:
         raise ValueError(f"tensors on different devices: {sorted(map(str, devices))}")
     return devices.pop()
-
-
-def _as_stream(stream, device):
-    import torch
-
-    if hasattr(stream, "cuda_stream"):
-        return stream
-    if int(stream) == 0:  # (an ExternalStream of handle 0 is a new stream)
-        return torch.cuda.default_stream(device)
-    return torch.cuda.ExternalStream(int(stream), device=device)
-
-
-def _hold(stream, *tensors):
-    """Tensors that a call on a stream other than the current one uses and hands
-    back: their memory is not reused before the stream is done with them."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(_as_stream(stream, t.device))
-
-
-def _empty(shape, dtype, device, stream, result=True):
-    """Memory for a call on `stream` (None: the current one), taken from that
-    stream's own: what the current stream has freed may still be in use by work it
-    has queued, which nothing orders before the call.  A `result` is handed back to
-    the current stream: it is not reused before that one is done with it, either."""
-    import torch
-
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    stream = _as_stream(stream, device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if result:
-        t.record_stream(torch.cuda.current_stream(device))
-    return t
 
 
 def _zeros_like(t, stream):

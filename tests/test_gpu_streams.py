@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2405_11143_amd as pda
+import workloads as W
 from test_gpu_fp8 import case, dev, up, upload  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +62,21 @@ def test_attention_over_the_8_bit_cache(dev, n):  # noqa: F811
                                              st.max_context_len, 48, num_query_tokens=n))["workspace_bytes"]
     call = lambda **more: pda.pda_decode_fp8(q, *on_gpu, table, lens, st.scale, **kw, **more)
     behind_pending_work(dev, [q.numel() * 4, need], lambda s: call(stream=s), call())
+
+
+@pytest.mark.parametrize("n", [1, 5])
+def test_attention_over_the_bf16_cache(dev, n):  # noqa: F811
+    st, cache, q, K, V = case([300, 77, 1, 250] * 10, 8, 2, 128, n, 31, dev)
+    k = W.k_rows_to_cache(up(K, dev, torch.bfloat16))
+    v, table, lens = up(V, dev, torch.bfloat16), up(st.block_table, dev), up(st.context_lens, dev)
+    prob = pda.make_problem(len(st.context_lens), 8, 2, 128, st.num_blocks, table.shape[1], st.max_context_len, 48,
+                            num_query_tokens=n)
+    call = lambda **more: pda.pda_decode(q, k, v, table, lens, st.scale, max_context_len=st.max_context_len,
+                                         partition_tokens=48, **more)
+    behind_pending_work(dev, [q.numel() * 4, pda.pda_workspace_bytes(prob)], lambda s: call(stream=s), call())
+
+
+def test_logprobs(dev):  # noqa: F811
+    logits, tokens = torch.randn(33, 40000, device=dev), torch.arange(33, dtype=torch.int32, device=dev)
+    call = lambda **more: pda.pda_token_logprobs(logits, tokens, **more)
+    behind_pending_work(dev, [33 * 4, 33 * 4, pda.pda.pda_logprob_workspace_bytes(33, 40000, 1)], lambda s: call(stream=s), call())

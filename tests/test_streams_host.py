@@ -108,6 +108,57 @@ def test_decode(monkeypatch, given, name):
     assert len(rec.made) == 2  # the output and the workspace
 
 
+def bf16_inputs(n=1):
+    q = torch.zeros(3, n, 4, 64, **bf)
+    return q, torch.zeros(8, 2, 8, 16, 8, **bf), torch.zeros(8, 2, 16, 64, **bf), torch.zeros(3, 4, **i32), torch.zeros(3, **i32)
+
+
+@pytest.mark.parametrize("name", ["bind_decode", "pda_decode", "pda_partition_attention", "bind_decode_append",
+                                  "pda_decode_append", "bind_decode_noalloc", "pda_decode_noalloc"])
+def test_bf16_step(monkeypatch, given, name):
+    q, k, v, table, lens = bf16_inputs()
+    new = torch.zeros(3, 1, 2, 64, **bf)
+    rec = Recorder(monkeypatch)
+    args = (q, new, new, k, v) if "append" in name else (q, k, v)
+    got = getattr(pda, name)(*args, table, lens, 0.125, max_context_len=64, partition_tokens=16, stream=given)
+    rec.check([got.result if name.startswith("bind") else got], cleared=False)
+    assert len(rec.made) == (1 if "noalloc" in name else 2)
+
+
+def test_bf16_shared_prefix(monkeypatch, given):
+    q, k, v, table, lens = bf16_inputs()
+    start, prefix = torch.tensor([0, 2], **i32), torch.tensor([16], **i32)
+    lib = pda.load_library()
+
+    class Library:  # (this one is not a bound call)
+        def __getattr__(self, name):
+            return (lambda *args: P.PDA_OK) if name == "pda_decode_shared_prefix" else getattr(lib, name)
+
+    rec = Recorder(monkeypatch)
+    monkeypatch.setattr(P, "load_library", Library)
+    out = pda.pda_decode_shared_prefix(q, k, v, table, lens, 0.125, start, prefix, max_context_len=64, max_group_size=2,
+                                       max_prefix_len=16, stream=given)
+    rec.check([out], cleared=False)
+    assert len(rec.made) == 2
+
+
+@pytest.mark.parametrize("name", ["bind_token_logprobs", "pda_token_logprobs"])
+def test_logprobs(monkeypatch, given, name):
+    logits, tokens = torch.zeros(5, 128256), torch.zeros(5, **i32)
+    rec = Recorder(monkeypatch)
+    got = getattr(pda, name)(logits, tokens, stream=given)
+    rec.check(got.result if name.startswith("bind") else got, cleared=False)
+    assert len(rec.made) == 3
+
+
+def test_ceilings(monkeypatch, given):
+    q, k, v, table, lens = bf16_inputs()
+    rec = Recorder(monkeypatch)
+    for call in (pda.bind_gather_ceiling(torch.zeros(4, **i32), k, v, 8, stream=given),
+                 pda.bind_stream_ceiling(k, 8, stream=given)):
+        rec.check([call.result], cleared=False)
+
+
 def test_without_a_stream_nothing_changes_it(monkeypatch):
     cache, table, lens = fp8_inputs()
     q = torch.zeros(3, 2, 4, 64, **bf)

@@ -494,6 +494,27 @@ def bind_append_kv(k_new, v_new, block_table, context_lens, k_cache, v_cache, *,
     return BoundCall("pda_append_kv", args, keep)
 
 
+class _MadeForGraph:
+    """Tensors allocated here for a captured graph, which is launched on any stream:
+    when it is made, nothing uses their memory any more, and that memory is not
+    reused before every stream it was launched on is done with it."""
+
+    def __init__(self, device, *tensors):
+        import torch
+
+        self._device, self._tensors, self._streams = device, [t for t in tensors if t is not None], set()
+        if self._tensors:
+            torch.cuda.current_stream(device).synchronize()
+
+    def stream_handle(self, stream):
+        """The handle of the stream (None: the current one) of a launch."""
+        handle = _stream_handle(stream, self._device)
+        if handle.value not in self._streams:
+            self._streams.add(handle.value)
+            _hold(handle.value or 0, *self._tensors)
+        return handle
+
+
 class ModelStepGraph:
     """pda_model_step_graph_create: a model's decode step over `layers` (a list
     of dicts with q, k_new, v_new, k_cache, v_cache and out tensors, one per
@@ -515,8 +536,10 @@ class ModelStepGraph:
                                        L["k_cache"].data_ptr(), L["v_cache"].data_ptr(), L["out"].data_ptr())
         L0 = layers[0]
         self.prob = _problem_from(L0["q"], L0["k_cache"], block_table, max_context_len, partition_tokens)
+        given = workspace
         workspace, ws_ptr, ws_bytes = _workspace(self.prob, workspace, L0["q"].device)
-        self.workspace, self._device = workspace, L0["q"].device
+        self._made = _MadeForGraph(L0["q"].device, workspace if given is None else None)
+        self.workspace = workspace
         self._keep = (layers, block_table, context_lens, arr)
         handle = ctypes.c_void_p()
         rc = load_library().pda_model_step_graph_create(
@@ -527,7 +550,7 @@ class ModelStepGraph:
         self._handle = handle
 
     def launch(self, stream=None):
-        rc = load_library().pda_step_graph_launch(self._handle, _stream_handle(stream, self._device))
+        rc = load_library().pda_step_graph_launch(self._handle, self._made.stream_handle(stream))
         if rc != PDA_OK:
             raise PdaError(rc, "pda_step_graph_launch")
 
@@ -554,12 +577,14 @@ class StepGraph:
                  max_context_len: int, partition_tokens: int = 0, workspace=None):
         import torch
 
+        given = out, workspace
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
         _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
         _check_new_kv(k_new, v_new, _query_shape(q), k_cache)
         self.prob = _problem_from(q, k_cache, block_table, max_context_len, partition_tokens)
         workspace, ws_ptr, ws_bytes = _workspace(self.prob, workspace, q.device)
+        self._made = _MadeForGraph(q.device, out if given[0] is None else None, workspace if given[1] is None else None)
         self.out, self.workspace = out, workspace
         self._keep = (q, k_new, v_new, k_cache, v_cache, block_table, context_lens)
         handle = ctypes.c_void_p()
@@ -572,7 +597,7 @@ class StepGraph:
         self._handle = handle
 
     def launch(self, stream=None):
-        rc = load_library().pda_step_graph_launch(self._handle, _stream_handle(stream, self.out.device))
+        rc = load_library().pda_step_graph_launch(self._handle, self._made.stream_handle(stream))
         if rc != PDA_OK:
             raise PdaError(rc, "pda_step_graph_launch")
         return self.out

@@ -80,3 +80,33 @@ def test_logprobs(dev):  # noqa: F811
     logits, tokens = torch.randn(33, 40000, device=dev), torch.arange(33, dtype=torch.int32, device=dev)
     call = lambda **more: pda.pda_token_logprobs(logits, tokens, **more)
     behind_pending_work(dev, [33 * 4, 33 * 4, pda.pda.pda_logprob_workspace_bytes(33, 40000, 1)], lambda s: call(stream=s), call())
+
+
+@pytest.mark.parametrize("model", [False, True])
+def test_captured_graphs(dev, model):  # noqa: F811
+    """A graph made behind pending work, whose class allocates the workspace (and the output), launched on another stream
+    at once."""
+    st, cache, q, K, V = case([300, 77, 1, 250] * 10, 8, 2, 128, 1, 31, dev)
+    k, v = W.k_rows_to_cache(up(K, dev, torch.bfloat16)), up(V, dev, torch.bfloat16)
+    table, lens = up(st.block_table, dev), up(st.context_lens, dev)
+    new = torch.randn(len(st.context_lens), 1, 2, 128, device=dev).to(torch.bfloat16)
+    kw = dict(max_context_len=st.max_context_len, partition_tokens=48)
+    pda.pda_append_kv(new, new, table, lens, k, v, max_context_len=st.max_context_len)
+    want = pda.pda_decode(q, k, v, table, lens, st.scale, **kw)
+    need = pda.pda_workspace_bytes(pda.make_problem(len(st.context_lens), 8, 2, 128, st.num_blocks, table.shape[1],
+                                                    st.max_context_len, 48))
+
+    def call(stream):
+        if model:
+            out = torch.zeros_like(want)
+            torch.cuda.synchronize()
+            graph = pda.ModelStepGraph([dict(q=q, k_new=new, v_new=new, k_cache=k, v_cache=v, out=out)], table, lens, st.scale,
+                                       **kw)
+            graph.launch(stream)
+        else:
+            graph = pda.StepGraph(q, new, new, k, v, table, lens, st.scale, **kw)
+            out = graph.launch(stream)
+        torch.cuda.synchronize()
+        return out
+
+    behind_pending_work(dev, [q.numel() * 4, need], call, want)

@@ -159,6 +159,44 @@ def test_ceilings(monkeypatch, given):
         rec.check([call.result], cleared=False)
 
 
+@pytest.mark.parametrize("model", [False, True])
+def test_graphs(monkeypatch, given, model):
+    """What a captured graph's class allocates is idle when the graph is made, and kept for every stream it is
+    launched on; tensors that are given are left alone."""
+    q, k, v, table, lens = bf16_inputs()
+    new = torch.zeros(3, 1, 2, 64, **bf)
+    lib = pda.load_library()
+
+    class Library:
+        def __getattr__(self, name):
+            return (lambda *args: P.PDA_OK) if "graph" in name else getattr(lib, name)
+
+    rec = Recorder(monkeypatch)
+    monkeypatch.setattr(P, "load_library", Library)
+    waits = []
+    monkeypatch.setattr(Stream, "synchronize", lambda s: waits.append(s.cuda_stream), raising=False)
+
+    def make(**kw):
+        if not model:
+            return pda.StepGraph(q, new, new, k, v, table, lens, 0.125, max_context_len=64, partition_tokens=16, **kw)
+        layer = dict(q=q, k_new=new, v_new=new, k_cache=k, v_cache=v, out=torch.zeros(3, 1, 4, 64))
+        kw.pop("out", None)
+        return pda.ModelStepGraph([layer], table, lens, 0.125, max_context_len=64, partition_tokens=16, **kw)
+
+    graph = make()
+    made = [graph.workspace] + ([] if model else [graph.out])
+    assert waits == [CURRENT] and {id(t) for t in made} == set(rec.made)
+    graph.launch(given)
+    graph.launch(given)
+    assert all(rec.kept[id(t)] == {SIDE} for t in made)
+    graph.launch()
+    assert all(rec.kept[id(t)] == {SIDE, CURRENT} for t in made)
+    rec.kept.clear()
+    mine = make(workspace=graph.workspace, out=torch.zeros(3, 1, 4, 64))
+    mine.launch(given)
+    assert waits == [CURRENT] and not rec.kept
+
+
 def test_without_a_stream_nothing_changes_it(monkeypatch):
     cache, table, lens = fp8_inputs()
     q = torch.zeros(3, 2, 4, 64, **bf)

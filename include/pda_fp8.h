@@ -18,7 +18,10 @@
  *   c_d = x_d * 2^(127 - s) rounded to the nearest e4m3 value, ties to even
  * A row of zeros has s = 0.  A row that holds a NaN or an infinity has s = 255
  * and NaN codes: it reads as NaN, and the attention's result is NaN in the rows that
- * see it, and in no others.  A power of two as the scale loses nothing
+ * see it, and in no others.  A value of 2^128 or more is an infinity (an element of
+ * 1.9375 * 2^127 or more rounds to one: code 256 under s = 247): it reads as one, and
+ * the attention's rows that see it hold what it makes of them, or NaN; no others
+ * change.  A power of two as the scale loses nothing
  * (the codes are floating point: whatever the scale, a value within 2^-15 of
  * the row's largest keeps its 4 bits), and both it and the codes' conversion
  * to bf16 are exact.  Elements below 2^-6 / 448 of the row's largest lose bits
@@ -38,7 +41,7 @@
  * All three 16-byte aligned.  A cache that a caller fills by itself follows the
  * same rules; larger scale bytes mean c_d * 2^(s - 127) too, and s = 0 zeros
  * whatever the codes (the attention takes them for c_d * 2^-127: below 2^-118).
- * NaN codes belong under s = 255 (under another byte they may also reach rows of
+ * NaN codes belong under s = 255 (under a byte below 247 they may also reach rows of
  * the same step that do not see them).
  * Slots past a context and blocks no sequence references are never
  * used, whatever they hold.

@@ -131,6 +131,18 @@ struct Codes {
   // Whether row e of the lane's four of V is one of NaN.
   __device__ __forceinline__ bool dead(int e) const { return (vs >> (8 * e) & 255u) == 255u; }
 
+  // Rows of V that hold an infinity become rows of NaN (their codes are in the 16 lanes of the k-group).
+  __device__ __forceinline__ void infinite_v(int kg) {
+    if (__builtin_amdgcn_ballot_w64((vs & (vs << 1) & 0x80808080u) != 0) == 0) return;  // (bytes of 192 and more)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint4& c = v[e / 2];
+      const unsigned s = vs >> (8 * e) & 255u;
+      const uint64_t hits = __builtin_amdgcn_ballot_w64(infinite(e % 2 ? c.z : c.x, s) || infinite(e % 2 ? c.w : c.y, s));
+      if (hits >> (16 * kg) & 0xffffu) vs |= 255u << (8 * e);
+    }
+  }
+
   // V's codes and scale bytes become zeros from row `rel` of the lane's four on, and
   // in the rows of NaN.
   __device__ __forceinline__ void clear_v(int rel) {
@@ -156,8 +168,8 @@ struct Fold : WaveAttention<D> {
   __device__ __forceinline__ Fold() : WA(0.f) {}
 
   // A zero probability would not keep a NaN of V from a row that does not see its
-  // token: in the tail, rows of NaN make the scores of the rows that see them NaN
-  // here, and are zeros in the product.
+  // token: in the tail, rows of NaN (and of infinities: infinite_v) make the scores of the
+  // rows that see them NaN here, and are zeros in the product.
   __device__ __forceinline__ void probabilities(const uint4 (&kr)[2][WA::NC], const Codes<D> (&c)[2], int tok0, int L,
                                                 int t_stop, bool tail, bf16x8_t (&part)[3]) {
     float sc[2][4];
@@ -197,6 +209,7 @@ template <int D, int NT>
 __device__ __forceinline__ void fold_pair(Fold<D> (&wave)[NT], Codes<D> (&c)[2], int tok0, int L, int l_first, int l_vis,
                                           int t_stop) {
   const bool tail = tok0 + 2 * kBlockTokens > min(l_first, t_stop);  // wavefront-uniform
+  if (tail) c[0].infinite_v(wave[0].kg), c[1].infinite_v(wave[0].kg);
   uint4 kr[2][WaveAttention<D>::NC];
   c[0].k_frags(kr[0]);
   c[1].k_frags(kr[1]);

@@ -110,6 +110,15 @@ __device__ __forceinline__ uint4 to_bf16(unsigned lo, unsigned hi, float factor)
   return make_uint4(two(lo, false), two(lo, true), two(hi, false), two(hi, true));
 }
 
+// Whether any of 4 codes stands for 2^128 or more under scale byte s (247 .. 254: codes
+// above that of 240 under 247, 120 under 248, ..; 255 is a row of NaN): an infinity as bf16.
+constexpr unsigned kLargeScale = 247;
+__device__ __forceinline__ bool infinite(unsigned codes, unsigned s) {
+  const unsigned top = 0x77u - 8u * (s - kLargeScale);
+  const unsigned m = codes & 0x7f7f7f7fu;
+  return s >= kLargeScale && ((m + (0x7fu - top) * 0x01010101u) & 0x80808080u) != 0;
+}
+
 // cos and sin of position * frequency (times sign), the angle in 64 bits:
 // whole turns are taken off before it is rounded to 32.
 __device__ __forceinline__ float2 turn(const RotaryArgs& r, int position, int pair) {

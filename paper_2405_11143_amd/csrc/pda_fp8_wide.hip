@@ -48,7 +48,7 @@ struct WideLds {
     f32x4_t o[W][kTileRows][D / 8];  // the epilogue, half of the columns at a time
   };
   int ids[window(W)];
-  unsigned char dead[buffers(W)][kStageBlocks * kBlockTokens];  // per token of a buffer: its values are NaN
+  unsigned char dead[buffers(W)][kStageBlocks * kBlockTokens];  // per token of a buffer: its values hold a NaN or an infinity
 };
 
 template <int D, int W>
@@ -197,14 +197,21 @@ wide_fp8_kernel(const DecodeFp8Args args) {
       const float f1 = is_k ? f0 : scale_of<1>(raw_scale[k]);
       uint4 lo = to_bf16(raw[k].x, raw[k].y, f0);
       uint4 hi = to_bf16(raw[k].z, raw[k].w, f1);
-      // A zero probability would not keep a NaN from a row that does not see its token:
-      // values past the context, whatever the slots hold, and rows of NaN are zeros
-      // there, and the latter make the scores of the rows that see them NaN (mask).
+      // A zero probability would not keep a NaN or an infinity from a row that does not see
+      // its token: values past the context, whatever the slots hold, and rows that hold one
+      // are zeros there, and the latter make the scores of the rows that see them NaN (mask).
       if (!is_k && tok0 + kStageBlocks * kBlockTokens > l_some) {
         asm volatile("");  // a branch
         const int blk = (k * kThreads + tid) / D % kStageBlocks;
         const int at = blk * kBlockTokens + s_off[k] - 16, t = tok0 + at;
-        const bool dead0 = (raw_scale[k] & 255u) == 255u, dead1 = (raw_scale[k] >> 8 & 255u) == 255u;
+        const unsigned s0 = raw_scale[k] & 255u, s1 = raw_scale[k] >> 8 & 255u;
+        bool dead0 = s0 == 255u, dead1 = s1 == 255u;
+        if (__builtin_amdgcn_ballot_w64(max(s0, s1) >= kLargeScale) != 0) {  // rows that hold an infinity: in RP lanes
+          const uint64_t h0 = __builtin_amdgcn_ballot_w64(infinite(raw[k].x, s0) || infinite(raw[k].y, s0));
+          const uint64_t h1 = __builtin_amdgcn_ballot_w64(infinite(raw[k].z, s1) || infinite(raw[k].w, s1));
+          const int first = lane / RP * RP;
+          dead0 |= (h0 >> first & ((1u << RP) - 1)) != 0, dead1 |= (h1 >> first & ((1u << RP) - 1)) != 0;
+        }
         if (t >= L || dead0) lo = make_uint4(0u, 0u, 0u, 0u);
         if (t + 1 >= L || dead1) hi = make_uint4(0u, 0u, 0u, 0u);
         st.dead[buffer][at] = dead0, st.dead[buffer][at + 1] = dead1;  // (the same from every thread of the row)

@@ -24,7 +24,8 @@
  * change.  A power of two as the scale loses nothing
  * (the codes are floating point: whatever the scale, a value within 2^-15 of
  * the row's largest keeps its 4 bits), and both it and the codes' conversion
- * to bf16 are exact.  Elements below 2^-6 / 448 of the row's largest lose bits
+ * to bf16 are exact (under s = 1 and 2 values are rounded to the nearest multiple of
+ * 2^-133, bf16's smallest).  Elements below 2^-6 / 448 of the row's largest lose bits
  * to e4m3's subnormals; a key's strong channels take nothing from the others
  * before that.
  *
@@ -149,7 +150,7 @@ int pda_decode_fp8(const pda_problem *prob, const void *q, const void *k_cache, 
                    const uint8_t *kv_scale, const int32_t *block_table, const int32_t *context_lens, float scale,
                    float *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Rows of the cache as bf16 (exact: a stored value has 4 significant bits).  Of
+/* Rows of the cache as bf16 (exact, as said above: a stored value has 4 significant bits).  Of
  * sequence b the tokens first_token[b], first_token[b] + 1, ... go to the rows
  * row_start[b] .. row_start[b + 1] - 1 of k_out and v_out
  * (bf16 [num_rows][num_kv_heads][D]), up to the end of its context; rows beyond that,

@@ -99,8 +99,9 @@ __device__ __forceinline__ float scale_of(unsigned bytes) {
   return __uint_as_float((up >= 0 ? bytes << (up & 31) : bytes >> (-up & 31)) & 0x7f800000u);
 }
 
-// 8 codes (two dwords) times a power of two, as 8 bf16: exact, and one
-// instruction for two of them.
+// 8 codes (two dwords) times a power of two, as 8 bf16, one instruction for two of them:
+// exact down to bf16's smallest, 2^-133 (values that are no multiples of it are rounded), and
+// infinite from 2^128 on.
 __device__ __forceinline__ uint4 to_bf16(unsigned lo, unsigned hi, float factor) {
   auto two = [&](unsigned w, bool upper) {
     const bf16x2_t x = upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, factor, true)

@@ -1,16 +1,85 @@
-"""Infinities in the 8-bit cache on the GPU: a stored value of 2^128 or more is one, and in
-the attention it reaches the rows that see its token and no others."""
+"""The ends of the 8-bit cache's range on the GPU: every code under every scale byte, rows
+whose largest value rounds up to 2^128, and values of that size in a cache that a caller
+filled.  A stored value of 2^128 or more is an infinity: it reads as one, and in the
+attention it reaches the rows that see its token and no others."""
 import numpy as np
 import pytest
+import torch
 
 import fp8_reference as ref
-from test_gpu_fp8 import case, decode, dev, f64, upload  # noqa: F401
+import paper_2405_11143_amd as pda
+import workloads as W
+from test_gpu_fp8 import case, decode, dev, download, f64, rounded, up, upload  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
 
 def stored(x):
     return np.where(np.abs(x) >= 2.0 ** 128, np.copysign(np.inf, x), x)
+
+
+def as_bf16(x):
+    """Values of 4 significant bits (or infinite) as bf16: those below 2^-126 rounded to its subnormals, ties to even."""
+    return np.where(np.abs(x) < 2.0 ** -126, np.rint(x * 2.0 ** 133) * 2.0 ** -133, x)
+
+
+def test_every_code_under_every_scale_byte(dev):  # noqa: F811
+    """Read back: exact from 2^-126 up (below, the nearest bf16 subnormal), infinite from 2^128 on; zeros under byte 0,
+    NaN under 255 and for NaN codes under the others."""
+    D, T = 64, 1024
+    cache = ref.empty_cache(T // 16, 1, D)
+    for t in range(T):  # token t: scale byte t / 4, codes 64 (t % 4) ..
+        for which in (0, 1):
+            ref.store(cache, t // 16, t % 16, which, (np.arange(64) + 64 * (t % 4)).astype(np.uint8)[None], np.array([t // 4]))
+    table, lens = up(np.arange(T // 16, dtype=np.int32)[None], dev), up(np.array([T], np.int32), dev)
+    out = torch.zeros(2, T, 1, D, dtype=torch.bfloat16, device=dev)
+    pda.pda_read_kv_fp8(*upload(cache, dev), table, lens, up(np.array([0, T], np.int32), dev), out[0], out[1], max_context_len=T)
+    s = np.arange(256)
+    want = as_bf16(stored(ref.VALUES * np.where(s == 255, 1.0, 2.0 ** (s - 127.0))[:, None]))
+    want[0], want[255] = 0.0, np.nan
+    for which in range(2):
+        assert np.array_equal(f64(out[which]).reshape(256, 256), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_near_the_largest_values(dev, D):  # noqa: F811
+    """Appended rows of finite values, up to the largest: elements of 1.9375 * 2^127 and more (which round to 2^128, as in
+    any format of 4 significant bits) read back infinite, the others within half a step."""
+    n, Hkv = 24, 2
+    st = W.custom_structure(1, Hkv, Hkv, D, [n], seed=3)
+    x = np.random.RandomState(D).uniform(-1, 1, (n, Hkv, D)) * 2.0 ** 127
+    top = torch.finfo(torch.bfloat16).max
+    x[0, :, 3], x[1, :, 5], x[2, :, 7], x[3, :, 9], x[4] = top, -top, 1.9375 * 2.0 ** 127, 1.9296875 * 2.0 ** 127, top
+    x = rounded(np.clip(x, -top, top), torch.bfloat16)
+    cache = upload(ref.empty_cache(st.num_blocks, Hkv, D), dev)
+    table, lens = up(st.block_table, dev), up(st.context_lens, dev)
+    new = up(x[None], dev, torch.bfloat16)
+    pda.pda_append_kv_fp8(new, new, table, lens, *cache, max_context_len=n)
+    out = torch.zeros(2, n, Hkv, D, dtype=torch.bfloat16, device=dev)
+    pda.pda_read_kv_fp8(*cache, table, lens, up(np.array([0, n], np.int32), dev), out[0], out[1], max_context_len=n)
+    bytes_ = download(cache)
+    t = np.arange(n)
+    for which in range(2):
+        got = f64(out[which])
+        assert np.array_equal(got, stored(ref.values(bytes_, which))[st.block_table[0, t // 16], :, t % 16])
+        over = np.abs(x) >= 1.9375 * 2.0 ** 127
+        assert np.array_equal(got[over], np.copysign(np.inf, x[over])) and over[2, :, 7].all() and not over[3].any()
+        f = ref.factor(bytes_[2][st.block_table[0, t // 16], :, which, t % 16])[..., None]
+        assert (np.abs(got - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * f))[~over].all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 20])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_context_of_one_token_at_the_smallest_scales(dev, D, n):  # noqa: F811
+    """The attention's rows are then V's, as bf16: subnormals too."""
+    for s in (1, 2, 3, 5, 9):
+        cache = ref.empty_cache(1, 1, D, fill=0)
+        ref.store(cache, 0, 0, 1, np.arange(D).astype(np.uint8)[None] * 2 % 128, np.array([s]))
+        q = torch.randn(1, n, 4, D, device=dev).to(torch.bfloat16)
+        one = up(np.ones(1, np.int32), dev)
+        got = pda.pda_decode_fp8(q, *upload(cache, dev), up(np.zeros((1, 1), np.int32), dev), one, 1.0, max_context_len=1)
+        want = as_bf16(ref.VALUES[np.arange(D) * 2 % 128] * 2.0 ** (s - 127))
+        assert np.array_equal(f64(got)[0, -1], np.broadcast_to(want, (4, D))) and (f64(got)[0, :-1] == 0).all()
 
 
 @pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 2), (128, 7, 1), (128, 4, 4)], ids=str)

@@ -134,7 +134,10 @@ int pda_append_kv_fp8(const pda_problem *prob, const pda_rotary *rotary, const v
                       const void *k_new, const void *v_new, const int32_t *block_table, const int32_t *context_lens,
                       void *k_cache, void *v_cache, uint8_t *kv_scale, hipStream_t stream);
 
-/* Plan of pda_decode_fp8 (its workspace differs from pda_decode's). */
+/* Plan of pda_decode_fp8 (its workspace differs from pda_decode's).  PDA_ERR_SHAPE also
+ * for what its launches cannot hold: 2^24 or more work items (partitions x sequences x KV
+ * heads x groups of up to 128 query rows), or more than 2^26 - 4 output rows where
+ * contexts are split. */
 int pda_plan_fp8(const pda_problem *prob, pda_plan_info *plan);
 
 /* pda_decode over this cache: the softmax attention of pda.h with

@@ -27,6 +27,7 @@ constexpr int64_t kPickItems = 3 * kAtOnce;
 constexpr int kWholeTokens = 2048;
 constexpr int64_t kWholePairs = 1, kWholeOf = 12;
 constexpr int64_t kMostItems = (1 << 24) - 1;  // workgroups of 256: a launch has less than 2^32 threads
+constexpr int64_t kMostMergeRows = 4 * kMostItems;  // the merge: workgroups of 256 for 4 rows
 constexpr int kMaxHeadDim = 512;  // of pda_rotary_apply
 
 bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr % a) == 0; }
@@ -82,6 +83,7 @@ int make_plan(const pda_problem* p, Plan* plan) {
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
   const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads * plan->tiles;
   if (pairs > kMostItems || parts * pairs > kMostItems) return PDA_ERR_SHAPE;
+  if (parts > 1 && (int64_t)p->num_seqs * n * p->num_q_heads > kMostMergeRows) return PDA_ERR_SHAPE;
   plan->items = parts * pairs;
   plan->slots = parts > 1 ? (size_t)p->num_seqs * n * p->num_q_heads * (size_t)parts : 0;
   plan->info.workspace_bytes = plan->slots * (p->head_dim + 2) * sizeof(float) + (size_t)plan->items * sizeof(int32_t);

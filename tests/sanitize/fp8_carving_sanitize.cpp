@@ -86,6 +86,7 @@ hipError_t launch_decode_fp8(const DecodeFp8Args& a, int head_dim, hipStream_t) 
 hipError_t launch_merge(const StepArgs& s, int, hipStream_t) {
   check_step(s);
   EXPECT(attended == 1 && s.part_o);
+  EXPECT((rows() + 3) / 4 * 256 < (int64_t)1 << 32);  // its threads: a wavefront per row, 4 to a workgroup
   ++merged;
   return hipSuccess;
 }

@@ -6,7 +6,8 @@
 // workgroup takes one token, forms its cosines and sines in LDS, a thread each,
 // and then its rows, 16 elements per thread.  16384 tokens of 32 + 8 heads of 128, bf16:
 // 59 us, 5.6 TB/s (a large copy 4.9); neighbouring pairs in half of 28 + 4 heads'
-// elements, the others copied: 47 us, 5.6 TB/s.  Four tokens to a workgroup (its loop
+// elements, the others copied: 47 us, 5.6 TB/s; in fp32, without the hint, 125 and 99 us, 5.3
+// TB/s.  Four tokens to a workgroup (its loop
 // goes from row to row and from token to token) took 8% longer than one, two 10%.
 #include "pda_fp8_internal.h"
 
@@ -33,6 +34,7 @@ __device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
 }
 template <bool NT>
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  static_assert(!NT, "bf16 rows only");
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
@@ -48,7 +50,7 @@ __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
     *reinterpret_cast<v8*>(p) = a;
 }
 
-// NT: stores with the non-temporal hint.
+// NT: stores with the non-temporal hint (bf16).
 template <typename T, bool NT>
 __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const RotaryApplyArgs a) {
   __shared__ float2 turns[kMaxPairs];
@@ -91,10 +93,13 @@ hipError_t launch_t(const RotaryApplyArgs& a, hipStream_t stream) {
   const int trips = (units + kMaxThreads - 1) / kMaxThreads;
   const int threads = min(kMaxThreads, ((units + trips - 1) / trips + kWaveSize - 1) / kWaveSize * kWaveSize);
   const dim3 grid(min(a.num_tokens, kMaxGrid));
-  if (sizeof(T) == 2 && a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim))
-    hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(threads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(threads), 0, stream, a);
+  if constexpr (sizeof(T) == 2) {
+    if (a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim)) {
+      hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(threads), 0, stream, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(threads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -80,7 +80,10 @@ typedef struct pda_rotary {
 } pda_rotary;
 
 /* Scaling of the frequencies f_i = base^(-2i / rotary_dim) for contexts longer
- * than those a model was trained on (original_len):
+ * than those a model was trained on (original_len), by published methods, to the letter
+ * (a model trained with one needs exactly its frequencies): position interpolation
+ * (arXiv 2306.15595), the "NTK-aware" change of the base, the wavelength bands of the
+ * Llama-3 family's long-context versions, and YaRN (arXiv 2309.00071):
  *   PLAIN   none
  *   LINEAR  f / factor: positions interpolated
  *   BASE    base * factor^(R / (R - 2)): the lowest frequency is divided by factor,

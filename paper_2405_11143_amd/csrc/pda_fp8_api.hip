@@ -10,20 +10,25 @@
 
 namespace {
 
-constexpr int64_t kAtOnce = 768;  // workgroups the GPU runs at once: 3 per compute unit
-// Ordered steps of at most this many items, and of pda::kPickPairs pairs, find their
-// items without the order kernel: a step of 256 sequences of 512-4096 tokens (2048 items)
+// Steps of more items than this run them sorted by size.  It is what the one-tile decode
+// kernel at head_dim 128 runs at once, 3 workgroups per compute unit; at 128 the two-tile
+// and the four-wavefront kernels run 512 and the two-wavefront one 1024 (at 64: one tile
+// 1024, two 768, four wavefronts 768, two 1536), where this line was not measured.
+constexpr int64_t kAtOnce = 768;
+// Sorted steps of at most this many items, and of pda::kPickPairs pairs, find their
+// items without the order kernel (one tile): a step of 256 sequences of 512-4096 tokens (2048 items)
 // takes 194.7 us instead of 197.7, 8 of up to 16384 (1152) 21.4 instead of 23.3.  Ranking costs
 // every workgroup about a microsecond: 16 of up to 16384 in 512s (3328 items) took
 // 42.5 instead of 36.7.
 constexpr int64_t kPickItems = 3 * kAtOnce;
-// Contexts up to this length stay whole where they all run at once and there are
-// kWholePairs (sequence, KV head) pairs for every kWholeOf tokens: a workgroup alone on a
+// Contexts of one-tile steps up to this length stay whole where they all run at once and
+// there are kWholePairs (sequence, KV head) pairs for every kWholeOf tokens: a workgroup alone on a
 // compute unit reads 2048 tokens in 13 us, and splitting costs a merge of 5, which
 // pays where most compute units would be idle.  Whole / the best of 256, 512 and 1024 in
 // us, 8 KV heads, contexts uniform up to the maximum: 24 sequences of 2048 16.6 / 17.8, 16
 // 16.8 / 13.9, 16 of 1500 13.6 / 13.4, 24 13.8 / 15.8, 16 of 1024 10.5 / 11.1, 8 10.5 /
-// 9.5; 64 of 2048 31.8 / 30.0, 48 26.4 / 25.7.
+// 9.5.  The rule has no line above, where whole contexts are a little slower: 48 of 2048
+// 26.4 / 25.7, 64 31.8 / 30.0.  Other numbers of KV heads and head_dim 64 were not measured.
 constexpr int kWholeTokens = 2048;
 constexpr int64_t kWholePairs = 1, kWholeOf = 12;
 constexpr int64_t kMostItems = (1 << 24) - 1;  // workgroups of 256: a launch has less than 2^32 threads
@@ -238,7 +243,7 @@ int pda_decode_fp8(const pda_problem* prob, const void* q, const void* k_cache, 
     s.part_m = ws + plan.slots * prob->head_dim;
     s.part_l = ws + plan.slots * (prob->head_dim + 1);
   }
-  // when every item runs at once their order is irrelevant (and the grid's y and z must hold them)
+  // (unsorted items are a grid of three dimensions, whose y and z must hold them)
   const bool ordered = plan.items > kAtOnce;
   a.picks = ordered && plan.narrow && plan.items <= kPickItems &&
             (int64_t)prob->num_seqs * plan.info.num_partitions <= pda::kPickPairs;

@@ -3,9 +3,9 @@
 //
 // A work item is (partition of a context, sequence, KV head, group of 32 W query
 // rows); row r of a sequence and KV head is head r % G of its new token r / G, and each
-// of the workgroup's W wavefronts takes 32 of them.  Bound by the matrix cores:
-// 4 D flop per row and token, in bf16, with the probabilities in two halves (6 D
-// issued).  As in pda_wide.hip both products run transposed on MFMA
+// of the workgroup's W wavefronts takes 32 of them.  Bound by the matrix cores (54% busy
+// in large chunks) and vector issue (52%): 4 D flop per row and token, in bf16, with the
+// probabilities in two halves (6 D issued).  As in pda_wide.hip both products run transposed on MFMA
 // f32_32x32x16_bf16 (S^T = K Q^T, O^T = V^T P^T: the lane's 16 scores belong to
 // one row and are its P^T fragments), and the scores of the next 32 tokens are
 // formed while these are folded, one stretch without a branch.  What differs is

@@ -148,8 +148,9 @@ int pda_plan_fp8(const pda_problem *prob, pda_plan_info *plan);
  * Both products run on exactly converted values with fp32 sums, so the result is
  * that of a bf16 cache holding the stored values: to fp32 accuracy (3e-7 of its norm)
  * where n Hq / Hkv is at most 32, and 2.5e-6 of its norm beyond, where the probabilities
- * are kept to 16 bits or more.  out is
- * fp32 [B][n][Hq][D]; rows that see nothing are zero.  `workspace`: any contents,
+ * are kept to 16 bits or more.  Scores (scale * q . K * log2 e) are below 2^30 in
+ * magnitude: past that the references that probabilities are taken against are too coarse.
+ * out is fp32 [B][n][Hq][D]; rows that see nothing are zero.  `workspace`: any contents,
  * pda_plan_fp8()'s workspace_bytes, 16-byte aligned; calls that overlap on the GPU
  * need separate ones. */
 int pda_decode_fp8(const pda_problem *prob, const void *q, const void *k_cache, const void *v_cache,

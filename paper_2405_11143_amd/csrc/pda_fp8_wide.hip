@@ -130,8 +130,9 @@ wide_fp8_kernel(const DecodeFp8Args args) {
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   // The reference of a row's probabilities, exp2(s * scale - m_run): a whole number
   // at most 8 below the largest scaled score so far (nothing overflows, and nothing
-  // that counts underflows).  The difference is one fused operation on an exact
-  // reference, so scores of any size cancel.
+  // that counts underflows; past 2^24 a score's own rounding comes to that, up to 2^30 no more
+  // than 2^32 of a probability).  The difference is one fused operation on an exact
+  // reference, the same for all tokens, so large scores cancel.
   float m_run = -1e30f, l_run = 0.f;
 
   const int32_t* table_row = a.table + (size_t)b * a.max_blocks_per_seq;

@@ -9,6 +9,7 @@ import torch
 import fp8_reference as ref
 import paper_2405_11143_amd as pda
 import workloads as W
+from fp8_accuracy import path
 from test_gpu_fp8 import case, decode, dev, download, f64, rounded, up, upload  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -80,6 +81,32 @@ def test_a_context_of_one_token_at_the_smallest_scales(dev, D, n):  # noqa: F811
         got = pda.pda_decode_fp8(q, *upload(cache, dev), up(np.zeros((1, 1), np.int32), dev), one, 1.0, max_context_len=1)
         want = as_bf16(ref.VALUES[np.arange(D) * 2 % 128] * 2.0 ** (s - 127))
         assert np.array_equal(f64(got)[0, -1], np.broadcast_to(want, (4, D))) and (f64(got)[0, :-1] == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 20, 40])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("partition_tokens", [0, 16])
+def test_equal_scores_of_any_size_allowed(dev, D, n, partition_tokens):  # noqa: F811
+    """Equal scores, up to 2^30 in units of log 2 either way, give the mean of the values: up to 40 of them are summed and
+    divided in fp32 (40 + 2 roundings), under probabilities that are off by their parts' error."""
+    L = 40
+    V = np.random.RandomState(n).randint(0, 120, (L, D)).astype(np.uint8)
+    for scale, code, s in ((0.125, 0x38, 127), (0.125, 0x7E, 144), (0.7, 0x7E, 144), (0.7, 0x78, 146), (-0.7, 0x78, 146)):
+        size = 4 * abs(scale) * ref.VALUES[code] * 2.0 ** (s - 127) * np.log2(np.e)
+        assert size < 2.0 ** 30
+        cache = ref.empty_cache(3, 1, D, fill=0)
+        for t in range(L):
+            k = np.zeros((1, D), np.uint8)
+            k[0, 5] = code | 128
+            ref.store(cache, t // 16, t % 16, 0, k, np.array([s]))
+            ref.store(cache, t // 16, t % 16, 1, V[None, t], np.array([127]))
+        q = torch.full((1, n, 4, D), 4.0, dtype=torch.bfloat16, device=dev)
+        got = f64(pda.pda_decode_fp8(q, *upload(cache, dev), up(np.arange(3, dtype=np.int32)[None], dev),
+                                     up(np.array([L], np.int32), dev), scale, max_context_len=L, partition_tokens=partition_tokens))
+        for i in range(n):
+            seen = ref.VALUES[V[:L - n + 1 + i]]
+            bar = 42 * 2.0 ** -24 + path(n, 4)[1]
+            assert (np.abs(got[0, i] - seen.mean(0)) <= bar * np.abs(seen).mean(0)).all(), (scale, s, i)
 
 
 @pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 2), (128, 7, 1), (128, 4, 4)], ids=str)

@@ -133,7 +133,6 @@ struct Codes {
 
   // Rows of V that hold an infinity become rows of NaN (their codes are in the 16 lanes of the k-group).
   __device__ __forceinline__ void infinite_v(int kg) {
-    if (__builtin_amdgcn_ballot_w64((vs & (vs << 1) & 0x80808080u) != 0) == 0) return;  // (bytes of 192 and more)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint4& c = v[e / 2];
@@ -209,7 +208,10 @@ template <int D, int NT>
 __device__ __forceinline__ void fold_pair(Fold<D> (&wave)[NT], Codes<D> (&c)[2], int tok0, int L, int l_first, int l_vis,
                                           int t_stop) {
   const bool tail = tok0 + 2 * kBlockTokens > min(l_first, t_stop);  // wavefront-uniform
-  if (tail) c[0].infinite_v(wave[0].kg), c[1].infinite_v(wave[0].kg);
+  if (tail) {
+    const unsigned large = c[0].vs & (c[0].vs << 1) | c[1].vs & (c[1].vs << 1);  // the top bits of bytes of 192 and more
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64((large & 0x80808080u) != 0) != 0, 0)) c[0].infinite_v(wave[0].kg), c[1].infinite_v(wave[0].kg);
+  }
   uint4 kr[2][WaveAttention<D>::NC];
   c[0].k_frags(kr[0]);
   c[1].k_frags(kr[1]);

@@ -209,8 +209,9 @@ __device__ __forceinline__ void fold_pair(Fold<D> (&wave)[NT], Codes<D> (&c)[2],
                                           int t_stop) {
   const bool tail = tok0 + 2 * kBlockTokens > min(l_first, t_stop);  // wavefront-uniform
   if (tail) {
-    const unsigned large = c[0].vs & (c[0].vs << 1) | c[1].vs & (c[1].vs << 1);  // the top bits of bytes of 192 and more
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64((large & 0x80808080u) != 0) != 0, 0)) c[0].infinite_v(wave[0].kg), c[1].infinite_v(wave[0].kg);
+    const unsigned top = (c[0].vs & (c[0].vs << 1)) | (c[1].vs & (c[1].vs << 1));  // bit 7: a byte of 192 or more
+    const bool large = __builtin_amdgcn_ballot_w64((top & 0x80808080u) != 0) != 0;
+    if (__builtin_expect(large, 0)) c[0].infinite_v(wave[0].kg), c[1].infinite_v(wave[0].kg);
   }
   uint4 kr[2][WaveAttention<D>::NC];
   c[0].k_frags(kr[0]);

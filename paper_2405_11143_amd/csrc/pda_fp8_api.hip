@@ -39,25 +39,13 @@ bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr % a) == 0; }
 
 int query_tokens(const pda_problem* p) { return p->num_query_tokens > 0 ? p->num_query_tokens : 1; }
 
+using pda::check_rotary;
+using pda::rotary_args;
+
 // The descriptor's own errors (those of pda_plan).
 int check_problem(const pda_problem* p) {
   pda_plan_info info;
   return pda_plan(p, &info);
-}
-
-int check_rotary(const pda_rotary* r, int head_dim) {
-  if (!r->inv_freq) return PDA_ERR_NULL;
-  if (r->rotary_dim < 1 || r->rotary_dim > head_dim) return PDA_ERR_SHAPE;
-  if (r->rotary_dim % 16 != 0) return PDA_ERR_UNSUPPORTED;
-  if ((r->interleaved != 0 && r->interleaved != 1) || (r->backward != 0 && r->backward != 1) || !isfinite(r->magnitude))
-    return PDA_ERR_VALUE;
-  if (!aligned(r->inv_freq, 8)) return PDA_ERR_ALIGNMENT;
-  return PDA_OK;
-}
-
-pda::RotaryArgs rotary_args(const pda_rotary* r) {
-  if (!r) return pda::RotaryArgs{nullptr, 1.f, 1.f, 0, 0};
-  return pda::RotaryArgs{r->inv_freq, r->magnitude, r->backward ? -1.f : 1.f, r->rotary_dim, r->interleaved};
 }
 
 struct Plan {

@@ -2,6 +2,8 @@
 // (include/pda_fp8.h), between their host layer and their gfx950 kernels.
 #pragma once
 
+#include <math.h>
+
 #include "pda_fp8.h"
 #include "pda_internal.h"
 
@@ -85,6 +87,22 @@ constexpr int kFp8TileRows = 16;  // query rows of an MFMA tile of the decode ke
 // Query rows of a work item whose sequence and KV head has `rows` of them: one or
 // two tiles of the decode kernel, or the rows of a workgroup of the wide one.
 inline int fp8_item_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+// A rotary embedding's own errors, for rows of head_dim elements.
+inline int check_rotary(const pda_rotary* r, int head_dim) {
+  if (!r->inv_freq) return PDA_ERR_NULL;
+  if (r->rotary_dim < 1 || r->rotary_dim > head_dim) return PDA_ERR_SHAPE;
+  if (r->rotary_dim % 16 != 0) return PDA_ERR_UNSUPPORTED;
+  if ((r->interleaved != 0 && r->interleaved != 1) || (r->backward != 0 && r->backward != 1) || !isfinite(r->magnitude))
+    return PDA_ERR_VALUE;
+  if ((uintptr_t)r->inv_freq % 8 != 0) return PDA_ERR_ALIGNMENT;
+  return PDA_OK;
+}
+
+inline RotaryArgs rotary_args(const pda_rotary* r) {
+  if (!r) return RotaryArgs{nullptr, 1.f, 1.f, 0, 0};
+  return RotaryArgs{r->inv_freq, r->magnitude, r->backward ? -1.f : 1.f, r->rotary_dim, r->interleaved};
+}
 
 // ---- device helpers ----
 
@@ -173,6 +191,39 @@ __device__ __forceinline__ void rotate_share(const float2* turns, bool interleav
       p[e] = a * c.x - b * c.y, q[e] = b * c.x + a * c.y;
     }
   }
+}
+
+// 8 elements of a row as fp32; NT: stored with the non-temporal hint.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
+template <>
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+template <>
+__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
+  typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+  const v8 a = *reinterpret_cast<const v8*>(p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+}
+template <bool NT>
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  static_assert(!NT, "bf16 rows only");
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+template <bool NT>
+__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
+  typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+  v8 a;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = (__bf16)x[i];
+  if (NT)
+    __builtin_nontemporal_store(a, reinterpret_cast<v8*>(p));
+  else
+    *reinterpret_cast<v8*>(p) = a;
 }
 
 // Whether the stores of the rotated rows (bf16) cover whole cache lines of 128 bytes:

@@ -18,38 +18,6 @@ constexpr int kMaxThreads = 256;
 constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
 constexpr int kMaxPairs = 256;  // head_dim <= 512
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
-template <>
-__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
-  typedef __bf16 v8 __attribute__((ext_vector_type(8)));
-  const v8 a = *reinterpret_cast<const v8*>(p);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
-}
-template <bool NT>
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  static_assert(!NT, "bf16 rows only");
-  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-}
-template <bool NT>
-__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
-  typedef __bf16 v8 __attribute__((ext_vector_type(8)));
-  v8 a;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = (__bf16)x[i];
-  if (NT)
-    __builtin_nontemporal_store(a, reinterpret_cast<v8*>(p));
-  else
-    *reinterpret_cast<v8*>(p) = a;
-}
-
 // NT: stores with the non-temporal hint (bf16).
 template <typename T, bool NT>
 __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const RotaryApplyArgs a) {

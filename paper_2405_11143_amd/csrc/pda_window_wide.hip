@@ -1,0 +1,374 @@
+// Attention with a sliding window and sinks (include/pda_window.h) for more than 32 query rows of
+// a (sequence, KV head): chunked and fresh prefill, long drafts.
+//
+// The fold is that of pda_wide.hip (32-row tiles on MFMA f32_32x32x16_bf16, K and V tiles
+// from memory straight to LDS, a 32-token step folded while the next one's scores are
+// formed), over a list of steps: the sinks', then the window's.  A work item is
+// (partition of the list, sequence, KV head, group of up to 8 chunks), one workgroup
+// of 4 wavefronts of two chunks each; a wavefront leaves out the steps that none of
+// its rows sees.  The items of one (sequence, KV head) run on one XCD next to each
+// other: neighbouring groups see almost the same tokens, which then come from its L2.
+#include "pda_wide.h"
+#include "pda_window_internal.h"
+
+namespace pda {
+namespace {
+
+constexpr int kXcds = 8;
+constexpr int kStep = kStageBlocks * kBlockTokens;  // tokens
+static_assert(kStep == kWindowWideUnit && kWgChunks * 16 == kWindowWideRows, "the plan's units");
+
+template <int D>
+__global__ void __launch_bounds__(kWaves * kWaveSize) __attribute__((amdgpu_waves_per_eu(2)))
+window_wide_kernel(const WindowArgs a) {
+  using S = WideLds<D>;
+  constexpr int KS = D / 16;  // score MFMA k-steps
+  constexpr int VT = D / 32;  // output tiles of 32 columns
+  constexpr int kTileBytes = kBlockTokens * D * 2;
+  __shared__ __align__(16) S st;
+
+  const StepArgs& sa = a.step;
+  const int Hq = sa.num_q_heads, Hkv = sa.num_kv_heads, G = sa.group, n = sa.num_query_tokens;
+  const int per_pair = a.num_groups * sa.num_partitions;
+  const int slot = blockIdx.x / kXcds;
+  const int pair = slot / per_pair * kXcds + blockIdx.x % kXcds;  // b * Hkv + g
+  if (pair >= sa.num_seqs * Hkv) return;
+  const int gr = slot % per_pair % a.num_groups, p = slot % per_pair / a.num_groups;
+  const int g = pair % Hkv, b = pair / Hkv;
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWaveSize - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5;   // which half of the k-groups the lane holds
+  const int col = lane & 31;  // the lane's row of the tile
+
+  int L = sa.lens[b];
+  L = L < 0 ? 0 : (L > sa.max_context_len ? sa.max_context_len : L);
+  const int i0 = gr * a.group_tokens, i1 = min(n, i0 + a.group_tokens);
+  const WindowSpan span = window_span(L, n, i0, i1, a.window, a.sinks, kStep);
+  const int per_part = sa.partition_tokens / kStep;
+  const int parts = (span.count() + per_part - 1) / per_part;
+  auto out_row = [&](int i, int h) { return ((size_t)b * n + i) * Hq + (size_t)g * G + h; };
+  if (p >= parts) {
+    if (parts == 0 && p == 0)  // nothing to see
+      for (int x = tid; x < (i1 - i0) * G * (D / 4); x += kWaves * kWaveSize) {
+        const int r = x / (D / 4);
+        store_nt4(sa.out + out_row(i0 + r / G, r % G) * D + 4 * (x % (D / 4)), 0.f, 0.f, 0.f, 0.f);
+      }
+    return;
+  }
+
+  // ---- this wavefront's tile: the new tokens [t0, t1), in chunks of query_chunk ----
+  const int qc = sa.query_chunk;
+  const int ta = i0 + 2 * w * qc;
+  const bool active = ta < i1;
+  const int t0 = active ? ta : i0, t1 = min(i1, t0 + 2 * qc);
+  const int chunk0 = col < 16 || t0 + qc >= t1 ? t0 : t0 + qc;  // the lane's chunk
+  const int my_rows = min(qc, t1 - chunk0) * G;
+  const int my_r = (col & 15) % my_rows;  // lane rows past the chunk's last one repeat real rows
+  const int my_i = chunk0 + my_r / G;
+  const int up = L - n + 1 + my_i, low = window_start(up, a.window);
+  // of all rows of the tile
+  const int up_min = L - n + 1 + t0, up_max = L - n + t1;
+  const int low_min = window_start(up_min, a.window), low_max = window_start(up_max, a.window);
+  const int sinks = a.sinks;
+  auto sees = [&](int t) { return t < up && (t < sinks || t >= low); };
+  auto all_see = [&](int t) { return t < up_min && (t < sinks || t >= low_max); };
+  auto some_see = [&](int t) { return t < up_max && (t < sinks || t >= low_min); };
+  auto whole = [&](int t) { return t + kStep <= up_min && (t + kStep <= sinks || t >= low_max); };
+  auto wanted = [&](int t) { return active && t < up_max && (t < sinks || t + kStep > low_min); };
+
+  float scale = sa.scale_log2;
+  const unsigned flip = scale < 0.f ? 0x80008000u : 0u;
+  const unsigned keep = scale == 0.f ? 0u : 0xffffffffu;  // a zero scale: zero scores, whatever is masked
+  scale = keep ? fabsf(scale) : 1.f;
+  bf16x8_t q[KS];
+  {
+    const uint16_t* qp = sa.q + out_row(my_i, my_r % G) * D + 8 * hh;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      uint4 u = *reinterpret_cast<const uint4*>(qp + 16 * c);
+      u.x = (u.x ^ flip) & keep, u.y = (u.y ^ flip) & keep, u.z = (u.z ^ flip) & keep, u.w = (u.w ^ flip) & keep;
+      q[c] = __builtin_bit_cast(bf16x8_t, u);
+    }
+  }
+  f32x16_t o[VT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  // the running maximum before scaling, and scaled and rounded (as in pda_wide.hip)
+  float m_raw = fmaxf(-1e30f / scale, -__FLT_MAX__), m_run = mul_rounded(m_raw, scale), l_run = 0.f;
+
+  const char* kpool = reinterpret_cast<const char*>(sa.k) + (size_t)g * kTileBytes;
+  const char* vpool = reinterpret_cast<const char*>(sa.v) + (size_t)g * kTileBytes;
+  const int32_t* table_row = sa.table + (size_t)b * sa.max_blocks_per_seq;
+  const size_t block_bytes = (size_t)Hkv * kTileBytes;
+  bool bad = false;  // a block id outside the pool, anywhere the item looks
+
+  // Staging, as in pda_wide.hip: 1 KiB of a tile per load instruction, K as it lies in
+  // memory, the 16-byte pieces of a V row permuted for the transposed reads.
+  constexpr int KPT = kTileBytes / 1024;
+  constexpr int kStepLoads = kStageBlocks * 2 * KPT / kWaves;  // per wavefront
+  constexpr int RP = D / 8;                                    // pieces of a V row
+  const int k_load = (w % KPT) * 1024 + lane * 16;
+  const int v_row = lane / RP;
+  const int v_load = (w % KPT) * 1024 + v_row * (2 * D) + 16 * ((lane % RP) ^ (D == 128 ? 4 * (v_row & 3) : 4 * ((v_row >> 1) & 1)));
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&st.buf[0][0][0]) +
+                        (w % KPT) * 1024;
+  int ids = 0;  // lane x: the id of block 64 (block / 64) + x of the ids held in LDS
+  auto issue = [&](int step) {
+    const int j = min(step * kStageBlocks, kWindow - kStageBlocks);  // steps past them load what nothing folds
+    if (j % kWaveSize == 0) ids = st.ids[j + lane];
+    const unsigned dst = lds0 + (step % kBuffers) * (kStageBlocks * S::kBlockPieces * 16);
+#pragma unroll
+    for (int s = 0; s < kStageBlocks; ++s) {
+      if (KPT * 2 == kWaves && (w >> 1) != s) continue;  // D = 64
+      const size_t off = (size_t)(unsigned)__builtin_amdgcn_readlane(ids, j % kWaveSize + s) * block_bytes;
+      const unsigned at = dst + s * (S::kBlockPieces * 16);
+      load_to_lds(kpool + off, k_load, at, vpool + off, v_load, at + kTileBytes);
+    }
+  };
+
+  typedef short v4s_t __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
+  const int k_piece = (col >> 4) * S::kBlockPieces + hh * 16 + (lane & 15);
+  const int s16 = lane & 15;
+  const int tr_row = (4 * hh + s16 / 4) * D + 16 * ((lane >> 4) & 1) + 4 * (s16 & 3);
+  int tr_off[VT];  // (with the row's permutation of pieces)
+#pragma unroll
+  for (int t = 0; t < VT; ++t) tr_off[t] = tr_row + 32 * (t ^ (D == 128 ? s16 / 4 : s16 / 8));
+
+  f32x16_t s;  // scores of the step to fold: reg i is token tok0 + 8 (i / 4) + 4 hh + i % 4
+  float top;   // the largest of them
+  auto scores = [&](const uint4* blocks) {
+    f32x16_t x;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < KS; ++c)
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, blocks[k_piece + 32 * c]), q[c], x, 0, 0, 0);
+    return x;
+  };
+  auto largest = [&] {
+    float x = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int i = 3; i + 1 < 15; i += 2) x = max3(x, s[i], s[i + 1]);
+    top = max3(x, s[15], s[15]);
+    asm volatile("" : "+v"(top));  // the MFMA results are first read in their own basic block
+  };
+  auto mask = [&](int tok0) {
+    if (!whole(tok0)) {  // wavefront-uniform: some row does not see some of these tokens
+      asm volatile("");  // a branch: as selects the masking would run on every step
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!sees(tok0 + 4 * hh + 8 * (i / 4) + i % 4)) s[i] = -__builtin_huge_valf();
+      largest();
+    }
+  };
+  // 0xffff for every half of x that is an infinity or NaN, as bf16
+  auto odd_halves = [](unsigned x) {
+    return ((x & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+  };
+  // Fold the step whose scores are in s (32 tokens from tok0 on, two blocks of
+  // a buffer), and form the scores of the next one (from next_tok0 on).
+  auto fold = [&](int tok0, const uint4* blocks, int next_tok0, const uint4* next_blocks) {
+    auto v_frag = [&](int m, int t) {
+      const uint16_t* v0 = reinterpret_cast<const uint16_t*>(blocks + S::kTilePieces + m * S::kBlockPieces) + tr_off[t];
+      const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)v0));
+      const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(v0 + 8 * D)));
+      return make_uint4(x.x, x.y, y.x, y.y);
+    };
+    uint4 vf[2][VT];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) vf[m][t] = v_frag(m, t);
+    if (!whole(tok0)) {  // wavefront-uniform
+      asm volatile("");
+      // Fragment words: tokens 4 hh + 16 m + {0, 2, 8, 10}, and the one after.  V rows that no row
+      // sees are zeroed, whatever they hold.  Infinities and NaN of tokens that only some rows see are left
+      // out, and counted for the rows that do see them, which become NaN there.
+      unsigned some[2][4], partly[2][4], mine[2][4];
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          some[m][h] = partly[m][h] = mine[m][h] = 0u;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int t = tok0 + 4 * hh + 16 * m + 8 * (h / 2) + 2 * (h % 2) + e;
+            const unsigned half = e ? 0xffff0000u : 0x0000ffffu;
+            some[m][h] |= some_see(t) ? half : 0u;
+            partly[m][h] |= some_see(t) && !all_see(t) ? half : 0u;
+            mine[m][h] |= sees(t) ? half & 0x3f803f80u : 0u;
+          }
+        }
+      bool odd = false;
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          vf[m][t].x &= some[m][0], vf[m][t].y &= some[m][1], vf[m][t].z &= some[m][2], vf[m][t].w &= some[m][3];
+          odd |= ((odd_halves(vf[m][t].x) & partly[m][0]) | (odd_halves(vf[m][t].y) & partly[m][1]) |
+                  (odd_halves(vf[m][t].z) & partly[m][2]) | (odd_halves(vf[m][t].w) & partly[m][3])) != 0;
+        }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          f32x16_t count;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            uint4& v = vf[m][t];
+            const uint4 out = make_uint4(odd_halves(v.x) & partly[m][0], odd_halves(v.y) & partly[m][1],
+                                         odd_halves(v.z) & partly[m][2], odd_halves(v.w) & partly[m][3]);
+            v = make_uint4(v.x & ~out.x, v.y & ~out.y, v.z & ~out.z, v.w & ~out.w);
+            constexpr unsigned kOnes = 0x3f803f80u;
+            count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8_t, make_uint4(out.x & kOnes, out.y & kOnes, out.z & kOnes, out.w & kOnes)),
+                __builtin_bit_cast(bf16x8_t, make_uint4(mine[m][0], mine[m][1], mine[m][2], mine[m][3])), count, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
+        }
+      }
+    }
+    float ref = m_run;
+    if (__builtin_amdgcn_ballot_w64(fmaf(top, scale, -m_run) > 8.f || fabsf(m_run) > kExactMax) != 0) {
+      const float mn = fmaxf(m_raw, fmaxf(top, __shfl_xor(top, 32)));
+      const float al = exp2_fast((m_raw - mn) * scale);
+      m_raw = mn;
+      m_run = mul_rounded(mn, scale);
+      ref = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] -= m_raw;
+      l_run *= al;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) o[t] *= al;
+    }
+    const f32x16_t ns = scores(next_blocks);
+    bf16x8_t bh[2], bl[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      float pr[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[i] = exp2_fast(fmaf(s[8 * m + i], scale, -ref));
+      l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+      unsigned hw[4], lw[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const unsigned h0 = __float_as_uint(pr[2 * h]) & 0xffff0000u;
+        const unsigned h1 = __float_as_uint(pr[2 * h + 1]) & 0xffff0000u;
+        hw[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        const bf16x2_t l2 = {(__bf16)(pr[2 * h] - __uint_as_float(h0)), (__bf16)(pr[2 * h + 1] - __uint_as_float(h1))};
+        lw[h] = __builtin_bit_cast(unsigned, l2);
+      }
+      bh[m] = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
+      bl[m] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        const bf16x8_t av = __builtin_bit_cast(bf16x8_t, vf[m][t]);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bh[m], o[t], 0, 0, 0);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bl[m], o[t], 0, 0, 0);
+      }
+    s = ns;
+    largest();
+    mask(next_tok0);
+  };
+
+  // the tokens that the item's rows see: block j of a step is needed if it holds one of them
+  const int end = L - n + i1, lo = window_start(L - n + i0 + 1, a.window);
+  auto needed = [&](int j) { return j * kBlockTokens < end && (j * kBlockTokens < sinks || (j + 1) * kBlockTokens > lo); };
+  const int v_end = min(span.count(), (p + 1) * per_part);
+  for (int vw = p * per_part; vw < v_end; vw += kWindow / kStageBlocks) {
+    const int nsteps = min(v_end - vw, kWindow / kStageBlocks);
+    // (as many as the steps and the loads issued past them read, by 64)
+    const int n_ids = min(kWindow, (nsteps * kStageBlocks + kBuffers * kStageBlocks + kWaveSize) / kWaveSize * kWaveSize);
+    for (int x = tid; x < n_ids; x += kWaves * kWaveSize) {
+      // past the end: the last step again (not folded); a step's block that nobody sees: the other one (masked)
+      const int j0 = span.token(vw + min(x / kStageBlocks, nsteps - 1), kStageBlocks) + x % kStageBlocks;
+      const int id = table_row[needed(j0) ? j0 : j0 ^ 1];
+      const bool ok = (unsigned)id < (unsigned)sa.num_blocks;  // never read outside the pool
+      bad |= !ok;
+      st.ids[x] = ok ? id : 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kBuffers - 1; ++x) issue(x);
+    bool ready = false;  // the scores of the step at hand are formed
+    for (int step = 0; step < nsteps; ++step) {
+      // the next step's loads of this wavefront, and behind the barrier those
+      // of the others; the last step's buffer is free then
+      wait_loads<(kBuffers - 3) * kStepLoads>();
+      __syncthreads();
+      issue(step + kBuffers - 1);
+      const int tok0 = span.token(vw + step, kStep), next = span.token(vw + step + 1, kStep);
+      if (!wanted(tok0)) {  // wavefront-uniform
+        ready = false;
+        continue;
+      }
+      if (!ready) {
+        s = scores(st.buf[step % kBuffers][0]);
+        largest();
+        mask(tok0);
+      }
+      fold(tok0, st.buf[step % kBuffers][0], next, st.buf[(step + 1) % kBuffers][0]);
+      ready = true;
+    }
+    wait_loads<0>();
+    __syncthreads();
+  }
+  const bool any_bad = __syncthreads_or(bad ? 1 : 0) != 0;  // (and the staging area is free)
+
+  l_run += __shfl_xor(l_run, 32);
+  const float mul = any_bad ? __builtin_nanf("") : parts == 1 && l_run > 0.f ? 1.f / l_run : 1.f;
+  const int swz = col & (D / 4 - 1);  // 16-byte units of a row permuted: conflict-free
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      st.o[w][col][(8 * t + 2 * k + hh) ^ swz] =
+          f32x4_t{o[t][4 * k] * mul, o[t][4 * k + 1] * mul, o[t][4 * k + 2] * mul, o[t][4 * k + 3] * mul};
+  __syncthreads();
+  if (!active) return;
+  for (int x = lane; x < kTileRows * (D / 4); x += kWaveSize) {
+    const int r32 = x / (D / 4);
+    const int d0 = 4 * (x % (D / 4));
+    const int c0 = r32 < 16 ? t0 : t0 + qc;  // the row's chunk
+    const int h = r32 & 15;
+    if (c0 >= t1 || h >= min(qc, t1 - c0) * G) continue;
+    const size_t row = out_row(c0 + h / G, h % G);
+    const f32x4_t v = st.o[w][r32][(d0 / 4) ^ (r32 & (D / 4 - 1))];
+    if (parts == 1)
+      store_nt4(sa.out + row * D + d0, v[0], v[1], v[2], v[3]);
+    else
+      *reinterpret_cast<f32x4_t*>(sa.part_o + (row * sa.slots_per_row + p) * D + d0) = v;
+  }
+  if (parts > 1 && hh == 0 && (col & 15) < my_rows && (col < 16 || t0 + qc < t1)) {
+    const size_t row = out_row(my_i, my_r % G);
+    sa.part_m[row * sa.slots_per_row + p] = m_run;
+    sa.part_l[row * sa.slots_per_row + p] = l_run;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_window_wide(const WindowArgs& a, int head_dim, hipStream_t stream) {
+  const unsigned pairs = (unsigned)a.step.num_seqs * (unsigned)a.step.num_kv_heads;
+  const dim3 grid((pairs + kXcds - 1) / kXcds * kXcds * (unsigned)a.num_groups * (unsigned)a.step.num_partitions);
+  const dim3 threads(kWaves * kWaveSize);
+  if (head_dim == 64)
+    hipLaunchKernelGGL(window_wide_kernel<64>, grid, threads, 0, stream, a);
+  else if (head_dim == 128)
+    hipLaunchKernelGGL(window_wide_kernel<128>, grid, threads, 0, stream, a);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace pda

@@ -1,4 +1,4 @@
-"""Python binding of the paged decode-attention C ABI (include/pda.h, include/pda_fp8.h).
+"""Python binding of the paged decode-attention C ABI (the headers under include/).
 
 Argument marshalling only: every step of the computation runs in the HIP
 kernels of libpda.so.  The library must have been built in-tree
@@ -30,7 +30,10 @@ EXPORTED = ("pda_plan", "pda_workspace_bytes", "pda_decode", "pda_partition_atte
             "pda_partition_attention_reusing_order", "pda_decode_noalloc",
             "pda_gather_ceiling", "pda_stream_ceiling", "pda_model_step_graph_create", "pda_decode_append",
             "pda_rotary_inv_freq", "pda_rotary_apply", "pda_append_kv_fp8", "pda_plan_fp8", "pda_decode_fp8",
-            "pda_read_kv_fp8", "pda_status_string")
+            "pda_read_kv_fp8",
+            "pda_norm_rotary", "pda_norm_rotary_workspace_bytes", "pda_norm_rotary_backward", "pda_norm_rotary_append",
+            "pda_plan_window", "pda_decode_window", "pda_blocks_workspace_bytes", "pda_blocks_resize", "pda_slot_map",
+            "pda_status_string")
 PDA_DTYPE_BF16, PDA_DTYPE_F32 = 0, 1
 PDA_ROTARY_PLAIN, PDA_ROTARY_LINEAR, PDA_ROTARY_BASE, PDA_ROTARY_BANDS, PDA_ROTARY_RAMP = 0, 1, 2, 3, 4
 
@@ -68,6 +71,30 @@ class pda_rotary(ctypes.Structure):
 class pda_rotary_scaling(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
                 ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class pda_head_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("weight_dtype", ctypes.c_int32),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class pda_rotary_axes(ctypes.Structure):
+    _fields_ = [("num_axes", ctypes.c_int32), ("axis_of_pair", ctypes.c_void_p), ("position_stride", ctypes.c_int64)]
+
+
+class pda_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("num_sinks", ctypes.c_int32)]
+
+
+class pda_block_pool(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("free_blocks", ctypes.c_void_p),
+                ("counts", ctypes.c_void_p)]
+
+
+class pda_token_rows(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int32), ("row_start", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p)]
 
 
 class PdaError(RuntimeError):
@@ -125,6 +152,18 @@ def load_library(path: str = LIB_PATH):
     lib.pda_plan_fp8.argtypes = [P, ctypes.POINTER(pda_plan_info)]
     lib.pda_decode_fp8.argtypes = [P, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
     lib.pda_read_kv_fp8.argtypes = [P] + [vp] * 7 + [c32, vp, vp, vp]
+    N, A = ctypes.POINTER(pda_head_norm), ctypes.POINTER(pda_rotary_axes)
+    lib.pda_norm_rotary.argtypes = [N, R, A, c32, c32, c32, c32, c32, vp] + [vp, c64] * 4 + [vp]
+    lib.pda_norm_rotary_workspace_bytes.argtypes = [c32, c32, c32, c32, ctypes.POINTER(sz)]
+    lib.pda_norm_rotary_backward.argtypes = [N, R, A, c32, c32, c32, c32, c32, vp] + [vp, c64] * 6 + [vp, vp, vp, sz, vp]
+    lib.pda_norm_rotary_append.argtypes = [N, R, A, c32, c32, c32, c32, c32, vp, vp] + [vp, c64] * 4 + [vp, vp, vp]
+    W = ctypes.POINTER(pda_window)
+    lib.pda_plan_window.argtypes = [P, W, ctypes.POINTER(pda_plan_info)]
+    lib.pda_decode_window.argtypes = [P, W, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    BP, TR = ctypes.POINTER(pda_block_pool), ctypes.POINTER(pda_token_rows)
+    lib.pda_blocks_workspace_bytes.argtypes = [BP, ctypes.POINTER(sz)]
+    lib.pda_blocks_resize.argtypes = [BP, vp, TR, vp, sz, vp]
+    lib.pda_slot_map.argtypes = [c32, c32, c32, vp, vp, TR, vp]
     lib.pda_status_string.argtypes = [i32]
     lib.pda_status_string.restype = ctypes.c_char_p
     for name in EXPORTED[:-1]:
@@ -1063,3 +1102,435 @@ def pda_read_kv_fp8(k_cache, v_cache, kv_scale, block_table, context_lens, row_s
     """Rows of the 8-bit cache back as contiguous bf16.  See bind_read_kv_fp8."""
     return bind_read_kv_fp8(k_cache, v_cache, kv_scale, block_table, context_lens, row_start, k_out, v_out,
                             max_context_len=max_context_len, first_token=first_token, stream=stream)()
+
+
+# ---- head norms, rotary positions with several axes, the append through a slot map
+# (include/pda_norm_rotary.h) ----
+
+def make_head_norm(q_weight=None, k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0) -> pda_head_norm:
+    """The norms of query and key heads: x / sqrt(mean x^2 + eps) * (weight +
+    weight_offset).  Weights are bf16 or float32 device tensors [D], both of one type; None:
+    no weights.  The result keeps them alive."""
+    import torch
+
+    given = [w for w in (q_weight, k_weight) if w is not None]
+    for w in given:
+        if w.dtype not in (torch.bfloat16, torch.float32) or w.dtype != given[0].dtype:
+            raise TypeError("the weights must be bfloat16 or float32, both the same")
+        _require("weight", w, w.dtype)
+        if w.dim() != 1:
+            raise ValueError("the weights must be [D]")
+    f32 = bool(given) and given[0].dtype == torch.float32
+    norm = pda_head_norm(float(eps), float(weight_offset), PDA_DTYPE_F32 if f32 else PDA_DTYPE_BF16,
+                         q_weight.data_ptr() if q_weight is not None else None,
+                         k_weight.data_ptr() if k_weight is not None else None)
+    norm.tensors = (q_weight, k_weight)
+    return norm
+
+
+def make_rotary_axes(axis_of_pair, num_axes: int) -> pda_rotary_axes:
+    """Positions on several axes: pair i turns by the position on axis
+    axis_of_pair[i] (uint8 device tensor [rotary_dim / 2], kept alive by the result)."""
+    import torch
+
+    _require("axis_of_pair", axis_of_pair, torch.uint8)
+    if axis_of_pair.dim() != 1:
+        raise ValueError("axis_of_pair must be [rotary_dim / 2]")
+    axes = pda_rotary_axes(int(num_axes), axis_of_pair.data_ptr(), 0)
+    axes.tensor = axis_of_pair
+    return axes
+
+
+def _head_call(positions, T, D, norm, rotary, axes):
+    """Checks what the calls below share; returns (pointers to norm, rotary and axes,
+    their tensors, what has to stay alive)."""
+    import torch
+
+    if T > 0x7fffffff:
+        raise ValueError("more than 2^31 - 1 tokens")
+    if positions.dtype != torch.int32:
+        raise TypeError(f"positions must be torch.int32, got {positions.dtype}")
+    if not positions.is_cuda:
+        raise ValueError("positions must be a device tensor")
+    tensors = [positions]
+    if norm is not None:
+        for w in norm.tensors:
+            if w is not None and w.shape != (D,):
+                raise ValueError(f"the norms' weights must be [{D}]")
+        tensors += [w for w in norm.tensors if w is not None]
+    if rotary is not None:
+        tensors.append(rotary.tensor)
+    if axes is None:
+        if positions.shape != (T,) or not positions.is_contiguous():
+            raise ValueError("positions must be [T], contiguous")
+    else:
+        if rotary is None:
+            raise ValueError("axes without rotary")
+        if axes.tensor.shape != rotary.tensor.shape:
+            raise ValueError("axis_of_pair must be [rotary_dim / 2]")
+        if positions.shape != (axes.num_axes, T) or (T > 1 and positions.stride(1) != 1):
+            raise ValueError("positions must be [num_axes][T]")
+        tensors.append(axes.tensor)
+        # (this call's own copy: the stride is that of its positions; that of a single axis is free)
+        axes = pda_rotary_axes(axes.num_axes, axes.axis_of_pair, positions.stride(0) if axes.num_axes > 1 else T)
+    ref = lambda x: ctypes.byref(x) if x is not None else None
+    return [ref(norm), ref(rotary), ref(axes)], tensors, (norm, rotary, axes, positions, tensors)
+
+
+def _head_rows(q, k):
+    import torch
+
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("q must be bfloat16 or float32")
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2])):
+        raise ValueError("q [T][Hq][D], k [T][Hkv][D]")
+    return PDA_DTYPE_BF16 if q.dtype == torch.bfloat16 else PDA_DTYPE_F32
+
+
+def _row_args(pairs):
+    """Pointers and token strides of (name, rows or None, dtype), ..."""
+    out = []
+    for name, t, dtype in pairs:
+        out += [None, 0] if t is None else [t.data_ptr(), _token_rows(name, t, dtype)]
+    return out
+
+
+def bind_norm_rotary(q, positions, k=None, norm: pda_head_norm = None, rotary: pda_rotary = None,
+                     axes: pda_rotary_axes = None, q_out=None, k_out=None, stream=None) -> DeviceCall:
+    """pda_norm_rotary bound to these tensors and the given (else the current)
+    stream; calling it returns (q_out, k_out).  q [T][Hq][D] and k [T][Hkv][D] are
+    bf16 or float32 with any token stride; the outputs are allocated when not
+    given, and may be the inputs (in place).  positions int32 [T], with `axes`
+    [num_axes][T]; negative (on the first axis): padding, left alone."""
+    dtype = _head_rows(q, k)
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    # (padding rows are not written: an output made here holds zeros there)
+    q_out = _zeros_like(q, stream) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = _zeros_like(k, stream)
+    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
+        raise ValueError("the outputs must have the inputs' shapes")
+    T, Hq, D = q.shape
+    heads, tensors, keep = _head_call(positions, T, D, norm, rotary, axes)
+    device = _same_device(q, q_out, k, k_out, *tensors)
+    rows = _row_args([("q", q, q.dtype), ("q_out", q_out, q.dtype), ("k", k, q.dtype), ("k_out", k_out, q.dtype)])
+    args = (*heads, T, Hq, 0 if k is None else k.shape[1], D, dtype, positions.data_ptr(), *rows,
+            _stream_handle(stream, device))
+    return DeviceCall("pda_norm_rotary", args, (keep, q, q_out, k, k_out), device, (q_out, k_out))
+
+
+def pda_norm_rotary(q, positions, k=None, norm: pda_head_norm = None, rotary: pda_rotary = None,
+                    axes: pda_rotary_axes = None, q_out=None, k_out=None, stream=None):
+    """Norms and rotary positions of q (and k) rows in one pass; returns (q_out, k_out
+    or None).  See bind_norm_rotary."""
+    result = bind_norm_rotary(q, positions, k, norm, rotary, axes, q_out, k_out, stream)()
+    _hold(stream, *result)
+    return result
+
+
+def pda_norm_rotary_workspace_bytes(num_tokens: int, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
+    import torch  # noqa: F401  (before the library: its HIP runtime is the one to share)
+
+    ws = ctypes.c_size_t()
+    rc = load_library().pda_norm_rotary_workspace_bytes(int(num_tokens), int(num_q_heads), int(num_kv_heads),
+                                                        int(head_dim), ctypes.byref(ws))
+    if rc != PDA_OK:
+        raise PdaError(rc, "pda_norm_rotary_workspace_bytes")
+    return ws.value
+
+
+def _given_workspace(workspace, need, device, stream):
+    """(workspace, pointer, bytes): the caller's, or one made here."""
+    import torch
+
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    if workspace is None and need > 0:
+        workspace = _empty((need,), torch.uint8, device, stream, result=False)
+    if workspace is None:
+        return None, None, 0
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def bind_norm_rotary_backward(q, q_grad, positions, k=None, k_grad=None, norm: pda_head_norm = None,
+                              rotary: pda_rotary = None, axes: pda_rotary_axes = None, dq=None, dk=None,
+                              dq_weight=None, dk_weight=None, workspace=None, stream=None) -> DeviceCall:
+    """pda_norm_rotary_backward bound to these tensors and the given (else the current)
+    stream: q and k are the inputs of pda_norm_rotary, q_grad and k_grad the
+    gradients of its outputs, `rotary` the forward's.  Calling it returns (dq, dk,
+    dq_weight, dk_weight); they are allocated when not given (the weights' gradients, float32
+    [D], for the weights that `norm` has).  dq may be q or q_grad, dk k or k_grad."""
+    import torch
+
+    dtype = _head_rows(q, k)
+    if norm is None:
+        raise ValueError("norm must be given (the gradient of the rotation alone: pda_norm_rotary with a backward rotary)")
+    if (k is None) != (k_grad is None) or (k is None and (dk is not None or dk_weight is not None)):
+        raise ValueError("k and k_grad go together")
+    T, Hq, D = q.shape
+    dq = _zeros_like(q, stream) if dq is None else dq
+    if k is not None and dk is None:
+        dk = _zeros_like(k, stream)
+    for t, like in ((q_grad, q), (dq, q), (k_grad, k), (dk, k)):
+        if t is not None and t.shape != like.shape:
+            raise ValueError("gradients must have the rows' shapes")
+    if dq_weight is None and norm.tensors[0] is not None:
+        dq_weight = _empty((D,), torch.float32, q.device, stream)
+    if k is not None and dk_weight is None and norm.tensors[1] is not None:
+        dk_weight = _empty((D,), torch.float32, q.device, stream)
+    for name, t in (("dq_weight", dq_weight), ("dk_weight", dk_weight)):
+        if t is not None:
+            _require(name, t, torch.float32)
+            if t.shape != (D,):
+                raise ValueError(f"{name} must be [{D}]")
+    heads, tensors, keep = _head_call(positions, T, D, norm, rotary, axes)
+    device = _same_device(q, q_grad, dq, k, k_grad, dk, dq_weight, dk_weight, workspace, *tensors)
+    Hkv = 0 if k is None else k.shape[1]
+    workspace, ws_ptr, ws_bytes = _given_workspace(workspace, pda_norm_rotary_workspace_bytes(T, Hq, Hkv, D), device, stream)
+    rows = _row_args([("q", q, q.dtype), ("q_grad", q_grad, q.dtype), ("dq", dq, q.dtype), ("k", k, q.dtype),
+                      ("k_grad", k_grad, q.dtype), ("dk", dk, q.dtype)])
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    args = (*heads, T, Hq, Hkv, D, dtype, positions.data_ptr(), *rows, ptr(dq_weight), ptr(dk_weight), ws_ptr, ws_bytes,
+            _stream_handle(stream, device))
+    call = DeviceCall("pda_norm_rotary_backward", args, (keep, q, q_grad, k, k_grad, workspace), device,
+                      (dq, dk, dq_weight, dk_weight))
+    call.workspace = workspace
+    return call
+
+
+def pda_norm_rotary_backward(q, q_grad, positions, k=None, k_grad=None, norm: pda_head_norm = None,
+                             rotary: pda_rotary = None, axes: pda_rotary_axes = None, dq=None, dk=None,
+                             dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """The gradient of pda_norm_rotary; returns (dq, dk, dq_weight, dk_weight).  See
+    bind_norm_rotary_backward."""
+    call = bind_norm_rotary_backward(q, q_grad, positions, k, k_grad, norm, rotary, axes, dq, dk, dq_weight, dk_weight,
+                                     workspace, stream)
+    result = call()
+    _hold(stream, *result, call.workspace)
+    return result
+
+
+def bind_norm_rotary_append(q, k, v, positions, slots, k_cache, v_cache, norm: pda_head_norm = None,
+                            rotary: pda_rotary = None, axes: pda_rotary_axes = None, q_out=None,
+                            stream=None) -> DeviceCall:
+    """pda_norm_rotary_append bound to these tensors and the given (else the current)
+    stream: k and v bf16 [T][Hkv][D] (k normed and rotated first) stored at slots[t] =
+    16 * block + place of the paged cache (k_cache, v_cache as in pda_decode), q bf16 [T][Hq][D] (or
+    None) normed and rotated into q_out (allocated when not given; may be q).  Calling it
+    returns q_out (None without q)."""
+    import torch
+
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _require(name, t, torch.bfloat16)
+    if k_cache.dim() != 5 or tuple(k_cache.shape[3:]) != (16, 8):
+        raise ValueError("k_cache must be [num_blocks][Hkv][D/8][16][8]")
+    NB, Hkv, C = k_cache.shape[:3]
+    if tuple(v_cache.shape) != (NB, Hkv, 16, 8 * C):
+        raise ValueError("v_cache must be [num_blocks][Hkv][16][D]")
+    for name, t in (("k", k), ("v", v), ("q", q)):
+        if t is not None and (t.dim() != 3 or t.shape[0] != k.shape[0] or t.shape[2] != 8 * C):
+            raise ValueError(f"{name} must be [T][heads][{8 * C}]")
+    if k.shape[1] != Hkv or v.shape[1] != Hkv:
+        raise ValueError("k, v and the caches disagree on the heads")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if q is not None and norm is None and rotary is None:
+        raise ValueError("q without norm and rotary has nothing to be done to it")
+    if q is not None:
+        q_out = _zeros_like(q, stream) if q_out is None else q_out
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    T, _, D = k.shape
+    _require("slots", slots, torch.int32)
+    if slots.shape != (T,):
+        raise ValueError("slots must be [T]")
+    heads, tensors, keep = _head_call(positions, T, D, norm, rotary, axes)
+    device = _same_device(q, q_out, k, v, slots, k_cache, v_cache, *tensors)
+    bf = torch.bfloat16
+    rows = _row_args([("q", q, bf), ("q_out", q_out, bf), ("k", k, bf), ("v", v, bf)])
+    args = (*heads, T, 0 if q is None else q.shape[1], Hkv, D, NB, positions.data_ptr(), slots.data_ptr(), *rows,
+            k_cache.data_ptr(), v_cache.data_ptr(), _stream_handle(stream, device))
+    return DeviceCall("pda_norm_rotary_append", args, (keep, q, q_out, k, v, slots, k_cache, v_cache), device, q_out)
+
+
+def pda_norm_rotary_append(q, k, v, positions, slots, k_cache, v_cache, norm: pda_head_norm = None,
+                           rotary: pda_rotary = None, axes: pda_rotary_axes = None, q_out=None, stream=None):
+    """Norms and rotary positions of packed tokens, their keys and values stored in the
+    paged cache; returns q_out (None without q).  See bind_norm_rotary_append."""
+    result = bind_norm_rotary_append(q, k, v, positions, slots, k_cache, v_cache, norm, rotary, axes, q_out, stream)()
+    _hold(stream, result)
+    return result
+
+
+# ---- attention with a sliding window and sinks (include/pda_window.h) ----
+
+def pda_plan_window(prob: pda_problem, window: int, sinks: int = 0) -> dict:
+    """The plan of pda_decode_window: partition_tokens, num_partitions, workspace_bytes."""
+    import torch  # noqa: F401  (before the library: its HIP runtime is the one to share)
+
+    info, w = pda_plan_info(), pda_window(int(window), int(sinks))
+    rc = load_library().pda_plan_window(ctypes.byref(prob), ctypes.byref(w), ctypes.byref(info))
+    if rc != PDA_OK:
+        raise PdaError(rc, "pda_plan_window")
+    return info.as_dict()
+
+
+def bind_decode_window(q, k_cache, v_cache, block_table, context_lens, scale: float, out=None, *, window: int,
+                       sinks: int = 0, max_context_len: int, partition_tokens: int = 0, workspace=None,
+                       stream=None) -> DeviceCall:
+    """pda_decode_window bound to these tensors and the given (else the current) stream:
+    the attention of bind_decode, of new tokens that see the last `window` tokens up to
+    their own, and the first `sinks`.  The other arguments are those of bind_decode
+    (`workspace`: pda_plan_window's workspace_bytes)."""
+    import torch
+
+    if out is None:
+        out = _empty(q.shape, torch.float32, q.device, stream)
+    if q.dim() == 4 and q.shape[1] == 0:
+        raise ValueError("at least one new token")
+    prob = _problem_from(q, k_cache, block_table, max_context_len, partition_tokens)
+    _check_tensors(q, k_cache, v_cache, block_table, context_lens, out)
+    device = _same_device(q, k_cache, v_cache, block_table, context_lens, out, workspace)
+    need = pda_plan_window(prob, window, sinks)["workspace_bytes"]
+    workspace, ws_ptr, ws_bytes = _given_workspace(workspace, need, device, stream)
+    w = pda_window(int(window), int(sinks))
+    args = (ctypes.byref(prob), ctypes.byref(w), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+            block_table.data_ptr(), context_lens.data_ptr(), ctypes.c_float(scale), out.data_ptr(), ws_ptr, ws_bytes,
+            _stream_handle(stream, device))
+    keep = (prob, w, q, k_cache, v_cache, block_table, context_lens, out, workspace)
+    call = DeviceCall("pda_decode_window", args, keep, device, out)
+    call.workspace = workspace
+    return call
+
+
+def pda_decode_window(q, k_cache, v_cache, block_table, context_lens, scale: float, out=None, *, window: int,
+                      sinks: int = 0, max_context_len: int, partition_tokens: int = 0, workspace=None, stream=None):
+    """One attention step with a sliding window and sinks; returns out (fp32, shaped like
+    q).  See bind_decode_window."""
+    call = bind_decode_window(q, k_cache, v_cache, block_table, context_lens, scale, out, window=window, sinks=sinks,
+                              max_context_len=max_context_len, partition_tokens=partition_tokens, workspace=workspace,
+                              stream=stream)
+    result = call()
+    _hold(stream, result, call.workspace)
+    return result
+
+
+# ---- block tables and slot maps on the GPU (include/pda_blocks.h) ----
+
+def make_block_pool(block_table, held, free_blocks, counts) -> pda_block_pool:
+    """A block pool of these int32 device tensors: block_table [num_seqs][max_blocks],
+    held [num_seqs], free_blocks [num_blocks] and counts [2] (include/pda_blocks.h); they are kept
+    alive by the result (`tensors`) and changed in place by pda_blocks_resize."""
+    import torch
+
+    for name, t in (("block_table", block_table), ("held", held), ("free_blocks", free_blocks), ("counts", counts)):
+        _require(name, t, torch.int32)
+    if block_table.dim() != 2 or held.shape != (block_table.shape[0],) or free_blocks.dim() != 1 or counts.shape != (2,):
+        raise ValueError("block_table [num_seqs][max_blocks], held [num_seqs], free_blocks [num_blocks], counts [2]")
+    pool = pda_block_pool(block_table.shape[0], free_blocks.shape[0], block_table.shape[1], block_table.data_ptr(),
+                          held.data_ptr(), free_blocks.data_ptr(), counts.data_ptr())
+    pool.tensors = (block_table, held, free_blocks, counts)
+    return pool
+
+
+def new_block_pool(num_seqs: int, num_blocks: int, max_blocks_per_seq: int, device="cuda") -> pda_block_pool:
+    """A pool whose rows hold nothing (entries -1) and whose blocks are all free,
+    block 0 on top of the stack."""
+    import torch
+
+    i32 = dict(dtype=torch.int32, device=device)
+    return make_block_pool(torch.full((num_seqs, max_blocks_per_seq), -1, **i32), torch.zeros(num_seqs, **i32),
+                           torch.arange(num_blocks - 1, -1, -1, **i32), torch.tensor([num_blocks, 0], **i32))
+
+
+def _token_map(num_seqs, row_start, positions, slots):
+    """(pda_token_rows or None, its tensors) of a slot map's tensors."""
+    import torch
+
+    given = [t for t in (positions, slots) if t is not None]
+    if not given:
+        if row_start is not None:
+            raise ValueError("row_start without positions or slots")
+        return None, ()
+    n = given[0].shape[0] if given[0].dim() == 1 else -1
+    for name, t in (("positions", positions), ("slots", slots)):
+        if t is not None:
+            _require(name, t, torch.int32)
+            if t.shape != (n,):
+                raise ValueError("positions and slots must be [num_rows], both the same")
+    if n > 0x7fffffff:
+        raise ValueError("more than 2^31 - 1 rows")
+    if row_start is not None:
+        _require("row_start", row_start, torch.int32)
+        if row_start.shape != (num_seqs + 1,):
+            raise ValueError("row_start must be [num_seqs + 1]")
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    return pda_token_rows(n, ptr(row_start), ptr(positions), ptr(slots)), (row_start, positions, slots)
+
+
+def _check_lens(context_lens, num_seqs):
+    import torch
+
+    _require("context_lens", context_lens, torch.int32)
+    if context_lens.shape != (num_seqs,):
+        raise ValueError("context_lens must be [num_seqs]")
+
+
+def bind_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, positions=None, slots=None, workspace=None,
+                       stream=None) -> DeviceCall:
+    """pda_blocks_resize bound to a pool (make_block_pool), lengths int32 [num_seqs] and the given
+    (else the current) stream: every row grown or shrunk to hold its length.  With positions
+    and/or slots (int32 [num_rows]) the slot map of the new tokens is written to them: row_start int32
+    [num_seqs + 1] says whose they are, None: the same number of every sequence.  Calling it returns
+    (block_table, positions, slots)."""
+    _check_lens(context_lens, pool.num_seqs)
+    rows, tensors = _token_map(pool.num_seqs, row_start, positions, slots)
+    device = _same_device(*pool.tensors, context_lens, workspace, *tensors)
+    ws = ctypes.c_size_t()
+    rc = load_library().pda_blocks_workspace_bytes(ctypes.byref(pool), ctypes.byref(ws))
+    if rc != PDA_OK:
+        raise PdaError(rc, "pda_blocks_workspace_bytes")
+    workspace, ws_ptr, ws_bytes = _given_workspace(workspace, ws.value, device, stream)
+    args = (ctypes.byref(pool), context_lens.data_ptr(), ctypes.byref(rows) if rows is not None else None, ws_ptr,
+            ws_bytes, _stream_handle(stream, device))
+    call = DeviceCall("pda_blocks_resize", args, (pool, context_lens, rows, tensors, workspace), device,
+                      (pool.tensors[0], positions, slots))
+    call.workspace = workspace
+    return call
+
+
+def pda_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, positions=None, slots=None, workspace=None,
+                      stream=None):
+    """Resizes a pool's rows for these lengths, in place, and writes the slot map of the
+    new tokens; returns (block_table, positions, slots).  See bind_blocks_resize."""
+    call = bind_blocks_resize(pool, context_lens, row_start, positions, slots, workspace, stream)
+    result = call()
+    _hold(stream, call.workspace)
+    return result
+
+
+def bind_slot_map(block_table, context_lens, num_blocks: int, row_start=None, positions=None, slots=None,
+                  stream=None) -> DeviceCall:
+    """pda_slot_map bound to these tensors and the given (else the current) stream: the
+    positions and slots of the new tokens of a block table however it was made.  Calling it returns
+    (positions, slots)."""
+    import torch
+
+    _require("block_table", block_table, torch.int32)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [num_seqs][max_blocks]")
+    B, width = block_table.shape
+    _check_lens(context_lens, B)
+    rows, tensors = _token_map(B, row_start, positions, slots)
+    if rows is None:
+        raise ValueError("positions or slots must be given")
+    device = _same_device(block_table, context_lens, *tensors)
+    args = (B, int(num_blocks), width, block_table.data_ptr(), context_lens.data_ptr(), ctypes.byref(rows),
+            _stream_handle(stream, device))
+    return DeviceCall("pda_slot_map", args, (block_table, context_lens, rows, tensors), device, (positions, slots))
+
+
+def pda_slot_map(block_table, context_lens, num_blocks: int, row_start=None, positions=None, slots=None, stream=None):
+    """Positions and slots of new tokens; returns (positions, slots).  See bind_slot_map."""
+    return bind_slot_map(block_table, context_lens, num_blocks, row_start, positions, slots, stream)()

@@ -128,8 +128,9 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const BlocksArgs a) 
   if (b == B) {  // rows of no sequence
     const int first = B > 0 ? (a.rows.row_start ? clamp_to(a.rows.row_start[0], n) : 0) : n;
     const int last = B > 0 ? (a.rows.row_start ? clamp_to(a.rows.row_start[B], n) : n) : n;
-    for (int64_t r = (int64_t)blockIdx.y * kMoveThreads + threadIdx.x; r < n; r += (int64_t)gridDim.y * kMoveThreads)
-      if (r < first || r >= last) write_row(a, r, -1, -1);
+    const int64_t step = (int64_t)gridDim.y * kMoveThreads, mine = (int64_t)blockIdx.y * kMoveThreads + threadIdx.x;
+    for (int64_t r = mine; r < first; r += step) write_row(a, r, -1, -1);
+    for (int64_t r = max(first, last) + mine; r < n; r += step) write_row(a, r, -1, -1);
     return;
   }
   int* const row = MOVE ? a.pool.block_table + (size_t)b * width : nullptr;

@@ -1,11 +1,15 @@
 // Head norms, rotary positions with several axes, the append through a slot map and the
 // gradient of the norms (include/pda_norm_rotary.h).
 //
-// All bound by memory: a row is read and written once (the gradient reads two).  As in
-// pda_rotary.hip a workgroup takes a token, forms the cosines and sines of its
-// positions in LDS, and then its rows, 16 elements per thread; a row's U threads are
-// neighbouring lanes, so its sum of squares is a few DPP steps.  A thread has two rows
-// in flight, loaded before the angles are formed.
+// All bound by memory: a row is read and written once (the gradient reads two).  A
+// wavefront takes a token, or with few tokens a part of one: it forms the cosines and sines of its
+// positions in its own corner of LDS, and then takes the rows, 64 / U at a time, 16 elements
+// per lane; a row's U lanes are neighbours, so its sum of squares is a few DPP steps.  The rows
+// of two steps are in flight, the first two loaded before the angles are formed.
+// Nothing waits for another wavefront.
+#include <algorithm>
+#include <type_traits>
+
 #include "pda_norm_rotary_internal.h"
 
 namespace pda {
@@ -16,6 +20,8 @@ constexpr int kWavesHere = kThreads / kWaveSize;
 constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
 constexpr int kMaxDim = 512;
 constexpr int kXcds = 8;
+constexpr int kFewWaves = 4096;    // wavefronts that fewer tokens are split into
+constexpr int kTwoTokens = 16384;  // tokens below this, and above the other, are split in two
 
 // 8 elements as they lie in memory.
 template <typename T>
@@ -56,229 +62,345 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// A thread's share of every row: as in pda_rotary.hip, or none at all for the lanes that fill
-// U up.
-__device__ __forceinline__ RowShare share_of(const RotaryArgs& r, int rotary_dim, int D, int u) {
-  return u < row_shares(D) ? row_share(r, rotary_dim, D, u) : RowShare{D, D, 0};
-}
+// What a lane has of every row: 16 elements as in pda_rotary.hip, or nothing (lanes that fill U up);
+// with the cosines and sines of the token at hand for them.
+struct Share {
+  int d0, d1, turned, D;
+  bool interleaved;
+  float c[8], s[8];  // half layout: of pair d0 + e; neighbouring pairs: of d0 / 2 + e and of d1 / 2 + e - 4
 
-template <typename T>
-struct RawShare {
-  Raw8<T> p, q;
-  __device__ __forceinline__ void load(const T* row, const RowShare& w, int D) {
-    if (w.d0 < D) p.load(row + w.d0);
-    if (w.d1 < D) q.load(row + w.d1);
+  __device__ __forceinline__ Share(const RotaryArgs& r, int R, int D_, int u) : D(D_), interleaved(r.interleaved) {
+    const RowShare w = u < row_shares(D) ? row_share(r, R, D, u) : RowShare{D, D, 0};
+    d0 = w.d0, d1 = w.d1, turned = w.turned;
   }
-  // (what the lane does not have counts as zeros)
-  __device__ __forceinline__ void floats(const RowShare& w, int D, float (&x)[8], float (&y)[8]) const {
+  __device__ __forceinline__ void read(const float2* turns) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
-    if (w.d0 < D) p.floats(x);
-    if (w.d1 < D) q.floats(y);
+    for (int e = 0; e < 8; ++e) {
+      if (turned == 0) continue;
+      if (interleaved && e >= 4 && turned < 2) continue;
+      const float2 t = turns[interleaved ? (e < 4 ? d0 / 2 + e : d1 / 2 + e - 4) : d0 + e];
+      c[e] = t.x, s[e] = t.y;
+    }
+  }
+  // Turns the lane's elements.
+  __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8]) const {
+    if (turned == 0) return;
+    auto pair = [&](float& a, float& b, int e) {
+      const float t = a;
+      a = t * c[e] - b * s[e], b = b * c[e] + t * s[e];
+    };
+    if (interleaved) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pair(x[2 * e], x[2 * e + 1], e);
+      if (turned == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pair(y[2 * e], y[2 * e + 1], 4 + e);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pair(x[e], y[e], e);
+    }
   }
 };
 
-// The lane's 16 weights of a norm, the offset added.
-__device__ __forceinline__ void load_weights(const NormRotaryArgs& a, int which, const RowShare& w, float (&x)[16]) {
-  const int D = a.head_dim;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = 1.f;
-  const void* p = a.weight[which];
-  if (!p) return;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int d = h ? w.d1 : w.d0;
-    if (d >= D) continue;
-    float y[8];
-    if (a.weight_f32)
-      load8(static_cast<const float*>(p) + d, y);
-    else
-      load8(static_cast<const __bf16*>(p) + d, y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[8 * h + i] = y[i] + a.offset;
+// A lane's elements of a row, as they lie in memory.  FULL: every lane has both vectors.
+template <typename T, bool FULL>
+struct RawShare {
+  Raw8<T> p, q;
+  // (`at` is the wavefront's, the byte offsets the lane's)
+  __device__ __forceinline__ void load(const char* at, bool has0, unsigned o0, bool has1, unsigned o1) {
+    if (FULL || has0) p.load(reinterpret_cast<const T*>(at + o0));
+    if (FULL || has1) q.load(reinterpret_cast<const T*>(at + o1));
   }
+  // (what the lane does not have counts as zeros)
+  __device__ __forceinline__ void floats(bool has0, bool has1, float (&x)[8], float (&y)[8]) const {
+    if (!FULL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
+    }
+    if (FULL || has0) p.floats(x);
+    if (FULL || has1) q.floats(y);
+  }
+};
+
+// The norms' weights of queries and of keys, the offset added, as fp32 in LDS.
+__device__ __forceinline__ void load_weights(const NormRotaryArgs& a, float (*weights)[kMaxDim]) {
+  for (int i = threadIdx.x; i < 2 * a.head_dim; i += blockDim.x) {
+    const int k = i < a.head_dim ? 0 : 1, d = i - k * a.head_dim;
+    const void* p = k == 0 ? a.weight[0] : a.weight[1];
+    float x = 1.f;
+    if (p) x = (a.weight_f32 ? static_cast<const float*>(p)[d] : (float)static_cast<const __bf16*>(p)[d]) + a.offset;
+    weights[k][d] = x;
+  }
+  __syncthreads();
 }
 
-// cos and sin of pair x of token t, whose position on the first axis is pos.
-__device__ __forceinline__ float2 turn_of(const NormRotaryArgs& a, int64_t t, int pos, int x) {
-  if (a.axis) {
-    const int axis = a.axis[x];
-    if (axis > 0 && axis < a.num_axes) pos = a.positions[axis * a.position_stride + t];
-  }
-  return turn(a.rot, pos, x);
+// LDS that the wavefront's lanes have written is theirs to read, and the other way round.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// What a row of the launch is.
+// The cosine and sine of every pair of token t, whose position on the first axis is pos, into the
+// wavefront's corner of LDS.
+__device__ __forceinline__ void form_turns(const NormRotaryArgs& a, int R, int64_t t, int pos, float2* turns) {
+  for (int i = threadIdx.x % kWaveSize; i < R / 2; i += kWaveSize) {
+    int p = pos;
+    if (a.axis) {
+      const int axis = a.axis[i];
+      if (axis > 0 && axis < a.num_axes) p = a.positions[axis * a.position_stride + t];
+    }
+    turns[i] = turn(a.rot, p, i);
+  }
+  wave_sync();
+}
+
+// A token's rows are taken by wavefronts, 64 / U of one kind at a time, so that what kind they
+// are, and where they lie, is the same for the wavefront.
 enum RowKind { kQuery = 0, kKey = 1, kValue = 2 };
+struct RowStep {
+  int kind, first;  // first head
+};
+__device__ __forceinline__ RowStep row_step(int i, int q_steps, int k_steps) {
+  const int kind = i < q_steps ? kQuery : i < q_steps + k_steps ? kKey : kValue;
+  return RowStep{kind, i - (kind == kQuery ? 0 : kind == kKey ? q_steps : q_steps + k_steps)};
+}
 
-// U: lanes per row.  NORM: the rows are normed.  STORE: keys and values go to the cache.  NT: the
-// queries go out with the non-temporal hint (and, without STORE, the keys).
-template <typename T, int U, bool NORM, bool STORE, bool NT>
-__global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryArgs a) {
-  __shared__ float2 turns[kMaxDim / 2];
-  const int D = a.head_dim;
+// U: lanes per row.  FULL: head_dim is 16 U.  NORM: the rows are normed.  STORE: keys and values go to the cache.  NT: the
+// queries go out with the non-temporal hint (and, without STORE, the keys).  `parts` wavefronts
+// share a token.
+template <typename T, int U, bool FULL, bool NORM, bool STORE, bool NT>
+__global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryArgs a, int parts) {
+  constexpr int RPW = kWaveSize / U;  // rows of a step
+  __shared__ float2 all_turns[kWavesHere][kMaxDim / 2];
+  __shared__ __align__(16) float weights[NORM ? 2 : 1][kMaxDim];
+  if constexpr (NORM) load_weights(a, weights);
+  const int D = FULL ? 16 * U : a.head_dim;
   const int R = a.rot.inv_freq ? a.rot.rotary_dim : 0;
-  const int u = threadIdx.x % U;
-  const int rows_at_once = blockDim.x / U;
-  const RowShare rotated = share_of(a.rot, R, D, u), plain = share_of(a.rot, 0, D, u);
+  const int lane = threadIdx.x % kWaveSize, u = lane % U, row = lane / U;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+  float2* const turns = all_turns[wave];
+  Share w(a.rot, R, D, u);
+  const int shares = row_shares(D);
+  const int v0 = 8 * u, v1 = 8 * (u + shares);  // of a row of values (STORE: every lane has both)
   const int nq = a.q.heads, nk = a.k.heads;
-  const int rows = nq + (STORE ? 2 : 1) * nk;
-  auto kind = [&](int h) { return h < nq ? kQuery : !STORE || h < nq + nk ? kKey : kValue; };
-  auto share = [&](int h) { return STORE && kind(h) == kValue ? plain : rotated; };
-  float wq[16], wk[16];
-  if (NORM) {
-    load_weights(a, 0, rotated, wq);
-    load_weights(a, 1, rotated, wk);
-  }
+  const int q_steps = (nq + RPW - 1) / RPW, k_steps = (nk + RPW - 1) / RPW;
+  const int steps = q_steps + (STORE ? 2 : 1) * k_steps;
   const float inv_d = 1.f / (float)D;
-  for (int64_t x = blockIdx.x; x < a.num_tokens; x += gridDim.x) {
+  const int d0 = w.d0, d1 = w.d1;
+  const bool has0 = d0 < D, has1 = d1 < D;
+  const unsigned row_at = row * D * (unsigned)sizeof(T);
+  for (int64_t x = (int64_t)blockIdx.x * kWavesHere + wave; x < (int64_t)a.num_tokens * parts;
+       x += (int64_t)gridDim.x * kWavesHere) {
     int64_t t = x;
-    if (STORE) {
-      // 16 neighbouring tokens, which fill whole lines of a block's keys together, on one XCD
-      const int64_t whole = a.num_tokens / (16 * kXcds) * (16 * kXcds);
-      if (x < whole) t = ((x / kXcds) / 16 * kXcds + x % kXcds) * 16 + (x / kXcds) % 16;
+    int part = 0;
+    if (parts > 1) {
+      t = (uint32_t)x / (uint32_t)parts;  // (few tokens)
+      part = (int)(x - t * parts);
+    } else if (STORE) {
+      // 16 neighbouring tokens, which fill whole lines of a block's keys together, on one XCD: 4
+      // workgroups, 8 numbers apart
+      constexpr int kRun = 16 * kXcds;
+      if (x < a.num_tokens / kRun * kRun) {
+        const int in = (int)(x % kRun), group = in / kWavesHere;
+        t = x - in + group % kXcds * 16 + group / kXcds * kWavesHere + in % kWavesHere;
+      }
     }
     const int pos = a.positions[t];
-    if (pos < 0) continue;  // padding (the whole workgroup)
+    if (pos < 0) continue;  // padding
     const int slot = STORE ? a.slots[t] : 0;
-    const bool stores = (unsigned)slot < 16u * (unsigned)a.num_blocks;
-    auto load = [&](int h, RawShare<T>& raw) {
-      const int which = kind(h);
-      const T* in = which == kQuery ? static_cast<const T*>(a.q.in) + t * a.q.in_stride + (int64_t)h * D
-                    : which == kKey ? static_cast<const T*>(a.k.in) + t * a.k.in_stride + (int64_t)(h - nq) * D
-                                    : reinterpret_cast<const T*>(a.v) + t * a.v_stride + (int64_t)(h - nq - nk) * D;
-      raw.load(in, share(h), D);
+    const uint64_t q_at = (uint64_t)(static_cast<const T*>(a.q.in) + t * a.q.in_stride);
+    const uint64_t k_at = (uint64_t)(static_cast<const T*>(a.k.in) + t * a.k.in_stride);
+    const uint64_t v_at = STORE ? (uint64_t)(reinterpret_cast<const T*>(a.v) + t * a.v_stride) : 0;
+    auto load = [=](int i, RawShare<T, FULL>& raw) __attribute__((always_inline)) {
+      if (i >= steps) return;
+      const RowStep s = row_step(i, q_steps, k_steps);
+      const int h = s.first * RPW + row;
+      const bool is_v = STORE && s.kind == kValue;
+      // (by arithmetic: selects of captured values would keep them in memory)
+      const int k = s.kind != kQuery, v = is_v;
+      const uint64_t at = q_at + k * (k_at - q_at) + v * (v_at - k_at) + s.first * (RPW * D * (int)sizeof(T));
+      if (h < nq + k * (nk - nq))
+        raw.load(reinterpret_cast<const char*>(at), has0, row_at + (d0 + v * (v0 - d0)) * (unsigned)sizeof(T), has1,
+                 row_at + (d1 + v * (v1 - d1)) * (unsigned)sizeof(T));
     };
-    auto finish = [&](int h, const RawShare<T>& raw) {
-      const int which = kind(h);
-      const RowShare w = share(h);
+    // A step's rows; `next` is loaded into its place.  Loads go out before the stores: waiting for a load waits
+    // for every store before it, too.
+    auto finish = [&](int i, RawShare<T, FULL>& raw, int next) __attribute__((always_inline)) {
+      if (i >= steps) return;
+      const RowStep s = row_step(i, q_steps, k_steps);
+      const int h = s.first * RPW + row;
+      const bool is_v = STORE && s.kind == kValue, is_q = s.kind == kQuery;
+      const RawShare<T, FULL> now = raw;
       float p[8], q[8];
-      raw.floats(w, D, p, q);
-      if (NORM) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(p[e], p[e], fmaf(q[e], q[e], s));
-        const float r = rsqrtf(fmaf(row_sum<U>(s), inv_d, a.eps));
-        if (!STORE || which != kValue) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] *= r * (which == kQuery ? wq[e] : wk[e]);
-            q[e] *= r * (which == kQuery ? wq[8 + e] : wk[8 + e]);
-          }
+      now.floats(has0, has1, p, q);
+      load(next, raw);
+      __builtin_amdgcn_sched_barrier(0);
+      if (h >= (is_q ? nq : nk)) return;  // (all lanes of a row together)
+      if constexpr (STORE) {
+        if (is_v) {
+          if ((unsigned)slot >= 16u * (unsigned)a.num_blocks) return;
+          char* at = reinterpret_cast<char*>(a.v_cache) +
+                     (((size_t)(slot / kBlockTokens) * nk + s.first * RPW) * kBlockTokens + slot % kBlockTokens) * (D * 2);
+          *reinterpret_cast<decltype(raw.p.x)*>(at + (row_at * kBlockTokens + v0 * 2u)) = now.p.x;
+          *reinterpret_cast<decltype(raw.q.x)*>(at + (row_at * kBlockTokens + v1 * 2u)) = now.q.x;
+          return;
         }
       }
-      rotate_share(turns, a.rot.interleaved, w, p, q);
-      if (STORE && which != kQuery) {
-        if (!stores) return;
-        const size_t tile = (size_t)(slot / kBlockTokens) * nk;
-        const int o = slot % kBlockTokens;
-        const size_t g = tile + (which == kKey ? h - nq : h - nq - nk);
-        __bf16* dst = reinterpret_cast<__bf16*>(which == kKey ? a.k_cache : a.v_cache);
-        auto at = [&](int d) { return which == kKey ? ((g * (D / 8) + d / 8) * kBlockTokens + o) * 8 : (g * kBlockTokens + o) * D + d; };
-        if (w.d0 < D) store8<false>(dst + at(w.d0), p);
-        if (w.d1 < D) store8<false>(dst + at(w.d1), q);
+      if constexpr (NORM) {
+        const float* wt = weights[is_q ? 0 : 1];
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(p[e], p[e], fmaf(q[e], q[e], ss));
+        const float r = rsqrtf(fmaf(row_sum<U>(ss), inv_d, a.eps));
+        const int w0 = FULL ? d0 : min(d0, D - 8), w1 = FULL ? d1 : min(d1, D - 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] *= r * wt[w0 + e], q[e] *= r * wt[w1 + e];
+      }
+      w.turn(p, q);
+      if (STORE && !is_q) {
+        if ((unsigned)slot >= 16u * (unsigned)a.num_blocks) return;
+        char* at = reinterpret_cast<char*>(a.k_cache) +
+                   ((size_t)(slot / kBlockTokens) * nk + s.first * RPW) * (D * kBlockTokens * 2) + slot % kBlockTokens * 16;
+        store8<false>(reinterpret_cast<__bf16*>(at + (row_at + d0 * 2u) * kBlockTokens), p);
+        store8<false>(reinterpret_cast<__bf16*>(at + (row_at + d1 * 2u) * kBlockTokens), q);
         return;
       }
-      T* out = which == kQuery ? static_cast<T*>(a.q.out) + t * a.q.out_stride + (int64_t)h * D
-                               : static_cast<T*>(a.k.out) + t * a.k.out_stride + (int64_t)(h - nq) * D;
-      if (w.d0 < D) store8<NT>(out + w.d0, p);
-      if (w.d1 < D) store8<NT>(out + w.d1, q);
+      char* out = reinterpret_cast<char*>(is_q ? static_cast<T*>(a.q.out) + t * a.q.out_stride : static_cast<T*>(a.k.out) + t * a.k.out_stride) +
+                  s.first * (RPW * D * (int)sizeof(T));
+      if (FULL || has0) store8<NT>(reinterpret_cast<T*>(out + (row_at + d0 * (unsigned)sizeof(T))), p);
+      if (FULL || has1) store8<NT>(reinterpret_cast<T*>(out + (row_at + d1 * (unsigned)sizeof(T))), q);
     };
-    RawShare<T> first, second;
-    int h = threadIdx.x / U;
-    if (h >= rows_at_once) h = rows;
-    if (h < rows) load(h, first);
-    if (h + rows_at_once < rows) load(h + rows_at_once, second);
-    for (int i = threadIdx.x; i < R / 2; i += blockDim.x) turns[i] = turn_of(a, t, pos, i);
-    __syncthreads();
-    while (h < rows) {  // (all lanes of a row together)
-      finish(h, first);
-      if (h + rows_at_once < rows) finish(h + rows_at_once, second);
-      h += 2 * rows_at_once;
-      if (h < rows) load(h, first);
-      if (h + rows_at_once < rows) load(h + rows_at_once, second);
+    RawShare<T, FULL> first, second;
+    load(part, first);
+    load(part + parts, second);
+    form_turns(a, R, t, pos, turns);
+    w.read(turns);
+    for (int i = part; i < steps; i += 2 * parts) {
+      finish(i, first, i + 2 * parts);
+      finish(i + parts, second, i + 3 * parts);
     }
-    __syncthreads();  // the next token's turns take the same place
+    wave_sync();  // the next token's turns take the same place
   }
 }
 
-// The gradient.  Every thread sums its elements' h u over its rows and tokens; at the end
-// the wavefronts' rows are summed by shuffles, the wavefronts through LDS.
-template <typename T, int U>
-__global__ void __launch_bounds__(kThreads) norm_rotary_grad_kernel(const NormRotaryArgs a) {
-  __shared__ float2 turns[kMaxDim / 2];
-  __shared__ float sums[kWavesHere][2][kMaxDim];
-  const int D = a.head_dim;
+// The gradient.  Every lane sums its elements' h u over its rows and tokens; at the end
+// the wavefront's rows are summed by shuffles, the wavefronts through LDS.
+template <typename T, int U, bool FULL>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) norm_rotary_grad_kernel(const NormRotaryArgs a) {
+  constexpr int RPW = kWaveSize / U;
+  __shared__ union {
+    float2 turns[kWavesHere][kMaxDim / 2];
+    float sums[kWavesHere][2][kMaxDim];
+  } lds;
+  __shared__ __align__(16) float weights[2][kMaxDim];
+  __shared__ f32x4_t key_sums[kWavesHere][4][kWaveSize];
+  load_weights(a, weights);
+  const int D = FULL ? 16 * U : a.head_dim;
   const int R = a.rot.inv_freq ? a.rot.rotary_dim : 0;
-  const int u = threadIdx.x % U;
-  const int rows_at_once = blockDim.x / U;
-  const RowShare w = share_of(a.rot, R, D, u);
-  const int nq = a.q.heads, rows = nq + a.k.heads;
-  float wq[16], wk[16], dwq[16], dwk[16];
-  load_weights(a, 0, w, wq);
-  load_weights(a, 1, w, wk);
+  const int lane = threadIdx.x % kWaveSize, u = lane % U, row = lane / U;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+  float2* const turns = lds.turns[wave];
+  Share w(a.rot, R, D, u);
+  const int nq = a.q.heads, nk = a.k.heads;
+  const int q_steps = (nq + RPW - 1) / RPW, steps = q_steps + (nk + RPW - 1) / RPW;
+  float dw[16];  // of queries; of keys, in LDS: with both in registers the kernel spills
 #pragma unroll
-  for (int e = 0; e < 16; ++e) dwq[e] = dwk[e] = 0.f;
+  for (int e = 0; e < 16; ++e) dw[e] = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) key_sums[wave][x][lane] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const float inv_d = 1.f / (float)D;
-  for (int64_t t = blockIdx.x; t < a.num_tokens; t += gridDim.x) {
+  const int d0 = w.d0, d1 = w.d1;
+  const bool has0 = d0 < D, has1 = d1 < D;
+  const unsigned row_at = row * D * (unsigned)sizeof(T);
+  for (int64_t t = (int64_t)blockIdx.x * kWavesHere + wave; t < a.num_tokens; t += (int64_t)gridDim.x * kWavesHere) {
     const int pos = a.positions[t];
-    if (pos < 0) continue;  // padding (the whole workgroup)
-    for (int i = threadIdx.x; i < R / 2; i += blockDim.x) turns[i] = turn_of(a, t, pos, i);
-    __syncthreads();
-    for (int h = threadIdx.x / U; h < rows; h += rows_at_once) {  // (all lanes of a row together)
-      const bool is_q = h < nq;
-      const RotaryRows& xr = is_q ? a.q : a.k;
-      const RotaryRows& gr = is_q ? a.q_grad : a.k_grad;
-      const int64_t at = (int64_t)(is_q ? h : h - nq) * D;
-      RawShare<T> xs, gs;
-      xs.load(static_cast<const T*>(xr.in) + t * xr.in_stride + at, w, D);
-      gs.load(static_cast<const T*>(gr.in) + t * gr.in_stride + at, w, D);
+    if (pos < 0) continue;  // padding
+    const uint64_t q_at = (uint64_t)(static_cast<const T*>(a.q.in) + t * a.q.in_stride);
+    const uint64_t k_at = (uint64_t)(static_cast<const T*>(a.k.in) + t * a.k.in_stride);
+    const uint64_t qg_at = (uint64_t)(static_cast<const T*>(a.q_grad.in) + t * a.q_grad.in_stride);
+    const uint64_t kg_at = (uint64_t)(static_cast<const T*>(a.k_grad.in) + t * a.k_grad.in_stride);
+    auto load = [=](int i, RawShare<T, FULL>& xs, RawShare<T, FULL>& gs) __attribute__((always_inline)) {
+      if (i >= steps) return;
+      const int k = i >= q_steps, first = i - k * q_steps;
+      if (first * RPW + row >= nq + k * (nk - nq)) return;
+      const int skip = first * (RPW * D * (int)sizeof(T));
+      const unsigned o0 = row_at + d0 * (unsigned)sizeof(T), o1 = row_at + d1 * (unsigned)sizeof(T);
+      xs.load(reinterpret_cast<const char*>(q_at + k * (k_at - q_at) + skip), has0, o0, has1, o1);
+      gs.load(reinterpret_cast<const char*>(qg_at + k * (kg_at - qg_at) + skip), has0, o0, has1, o1);
+    };
+    auto finish = [&](int i, RawShare<T, FULL>& xs, RawShare<T, FULL>& gs, int next) __attribute__((always_inline)) {  // (as above)
+      if (i >= steps) return;
+      const bool is_q = i < q_steps;
+      const int h = (is_q ? i : i - q_steps) * RPW + row;
       float p[8], q[8], gp[8], gq[8];
-      xs.floats(w, D, p, q);
-      gs.floats(w, D, gp, gq);
-      rotate_share(turns, a.rot.interleaved, w, gp, gq);
+      xs.floats(has0, has1, p, q);
+      gs.floats(has0, has1, gp, gq);
+      load(next, xs, gs);
+      __builtin_amdgcn_sched_barrier(0);
+      if (h >= (is_q ? nq : nk)) return;  // (all lanes of a row together)
+      float wp[8], wq[8];
+      int which = is_q ? 0 : 1;
+      asm volatile("" : "+v"(which));  // (read for every step: kept, the weights of both kinds would take 32 registers)
+      const float* wt = weights[which];
+      const int w0 = FULL ? d0 : min(d0, D - 8), w1 = FULL ? d1 : min(d1, D - 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wp[e] = wt[w0 + e], wq[e] = wt[w1 + e];
+      w.turn(gp, gq);
       float ss = 0.f, gx = 0.f;  // sums of x^2 and of f x
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
+        wp[e] *= gp[e], wq[e] *= gq[e];  // f
         ss = fmaf(p[e], p[e], fmaf(q[e], q[e], ss));
-        gx = fmaf(gp[e] * (is_q ? wq[e] : wk[e]), p[e], fmaf(gq[e] * (is_q ? wq[8 + e] : wk[8 + e]), q[e], gx));
+        gx = fmaf(wp[e], p[e], fmaf(wq[e], q[e], gx));
       }
       const float r = rsqrtf(fmaf(row_sum<U>(ss), inv_d, a.eps));
       const float c = row_sum<U>(gx) * r * inv_d;  // mean of f u
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float up = p[e] * r, uq = q[e] * r;
-        const float hp = gp[e] * up, hq = gq[e] * uq;
-        dwq[e] += is_q ? hp : 0.f, dwq[8 + e] += is_q ? hq : 0.f;
-        dwk[e] += is_q ? 0.f : hp, dwk[8 + e] += is_q ? 0.f : hq;
-        p[e] = r * fmaf(-up, c, gp[e] * (is_q ? wq[e] : wk[e]));
-        q[e] = r * fmaf(-uq, c, gq[e] * (is_q ? wq[8 + e] : wk[8 + e]));
+        p[e] *= r, q[e] *= r;  // u
+        gp[e] *= p[e], gq[e] *= q[e];
+        p[e] = r * fmaf(-p[e], c, wp[e]), q[e] = r * fmaf(-q[e], c, wq[e]);
       }
-      T* out = static_cast<T*>(xr.out) + t * xr.out_stride + at;
-      if (w.d0 < D) store8<false>(out + w.d0, p);
-      if (w.d1 < D) store8<false>(out + w.d1, q);
-    }
-    __syncthreads();  // the next token's turns take the same place
+      if (is_q) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[e] += gp[e], dw[8 + e] += gq[e];
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float* y = x < 2 ? gp + 4 * x : gq + 4 * (x - 2);
+          key_sums[wave][x][lane] += f32x4_t{y[0], y[1], y[2], y[3]};
+        }
+      }
+      char* out = reinterpret_cast<char*>(is_q ? static_cast<T*>(a.q.out) + t * a.q.out_stride : static_cast<T*>(a.k.out) + t * a.k.out_stride) +
+                  (is_q ? i : i - q_steps) * (RPW * D * (int)sizeof(T));
+      if (FULL || has0) store8<false>(reinterpret_cast<T*>(out + (row_at + d0 * (unsigned)sizeof(T))), p);
+      if (FULL || has1) store8<false>(reinterpret_cast<T*>(out + (row_at + d1 * (unsigned)sizeof(T))), q);
+    };
+    RawShare<T, FULL> xs, gs;
+    load(0, xs, gs);
+    form_turns(a, R, t, pos, turns);
+    w.read(turns);
+    for (int i = 0; i < steps; ++i) finish(i, xs, gs, i + 1);
+    wave_sync();  // the next token's turns take the same place
   }
+  __syncthreads();  // (the sums take the turns' place)
 #pragma unroll
-  for (int e = 0; e < 16; ++e)
-#pragma unroll
-    for (int m = U; m < kWaveSize; m <<= 1) {
-      dwq[e] += __shfl_xor(dwq[e], m);
-      dwk[e] += __shfl_xor(dwk[e], m);
-    }
-  const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
-  if (lane < U) {
+  for (int k = 0; k < 2; ++k) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int d = (e < 8 ? w.d0 : w.d1) + e % 8;
-      if (d < D) sums[wave][0][d] = dwq[e], sums[wave][1][d] = dwk[e];
+      float x = k == 0 ? dw[e] : key_sums[wave][e / 4][lane][e % 4];
+#pragma unroll
+      for (int m = U; m < kWaveSize; m <<= 1) x += __shfl_xor(x, m);
+      const int d = (e < 8 ? d0 : d1) + e % 8;
+      if (lane < U && d < D) lds.sums[wave][k][d] = x;
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += blockDim.x) {
+  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
     float s = 0.f;
-    for (int x = 0; x < (int)blockDim.x / kWaveSize; ++x) s += sums[x][i / D][i % D];
+#pragma unroll
+    for (int x = 0; x < kWavesHere; ++x) s += lds.sums[x][i / D][i % D];
     a.part[(size_t)blockIdx.x * 2 * D + i] = s;
   }
 }
@@ -290,7 +412,14 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const float* part
   __shared__ float s[kThreads / kSumColumns][kSumColumns];
   const int c = blockIdx.x * kSumColumns + threadIdx.x % kSumColumns, run = threadIdx.x / kSumColumns;
   float x = 0.f;
-  for (int i = run; i < groups; i += kThreads / kSumColumns) x += part[(size_t)i * 2 * D + c];
+  constexpr int kRuns = kThreads / kSumColumns, kAhead = 16;
+  for (int i = run; i < groups; i += kRuns * kAhead) {
+    float y[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) y[k] = i + k * kRuns < groups ? part[(size_t)(i + k * kRuns) * 2 * D + c] : 0.f;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) x += y[k];
+  }
   s[run][threadIdx.x % kSumColumns] = x;
   __syncthreads();
   if (run == 0) {
@@ -300,40 +429,53 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const float* part
   }
 }
 
-// A workgroup has as many threads as make its last trip through the rows a full one, nearly.
-int threads_for(int rows, int U) {
-  const int64_t units = (int64_t)rows * U;
-  const int64_t trips = (units + kThreads - 1) / kThreads;
-  return (int)min((int64_t)kThreads, ((units + trips - 1) / trips + kWaveSize - 1) / kWaveSize * kWaveSize);
+// Wavefronts that share a token: one where tokens are many, up to one for each of its steps where
+// they are few; as many as make the last trip a full one, nearly.
+int parts_of(int U, int64_t tokens, int q_heads, int key_heads, int value_heads) {
+  const int rpw = kWaveSize / U;
+  auto steps_of = [&](int heads) { return (heads + rpw - 1) / rpw; };
+  const int steps = steps_of(q_heads) + steps_of(key_heads) + steps_of(value_heads);
+  const int64_t ways = tokens > kFewWaves && tokens < kTwoTokens ? 2 : std::max<int64_t>(1, kFewWaves / tokens);
+  const int most = (int)std::min<int64_t>(steps, ways);
+  const int trips = (steps + most - 1) / most;
+  return (steps + trips - 1) / trips;
 }
 
-// f(integral_constant U): the lanes that a row of head_dim elements takes.
+unsigned grid_of(int64_t tokens, int parts) {
+  return (unsigned)std::min<int64_t>(kMaxGrid, (tokens * parts + kWavesHere - 1) / kWavesHere);
+}
+
+// f(U, FULL) as integral constants: the lanes that a row of head_dim elements takes.
 template <typename F>
 void with_lanes(int head_dim, F&& f) {
+  auto with = [&](auto lanes) {
+    head_dim == 16 * decltype(lanes)::value ? f(lanes, std::true_type()) : f(lanes, std::false_type());
+  };
   const int shares = row_shares(head_dim);
   if (shares <= 4)
-    f(std::integral_constant<int, 4>());
+    with(std::integral_constant<int, 4>());
   else if (shares <= 8)
-    f(std::integral_constant<int, 8>());
+    with(std::integral_constant<int, 8>());
   else if (shares <= 16)
-    f(std::integral_constant<int, 16>());
+    with(std::integral_constant<int, 16>());
   else
-    f(std::integral_constant<int, 32>());
+    with(std::integral_constant<int, 32>());
 }
 
 template <typename T, bool NORM>
 void launch_apply(const NormRotaryArgs& a, hipStream_t stream) {
-  const dim3 grid(min(a.num_tokens, kMaxGrid));
-  with_lanes(a.head_dim, [&](auto lanes) {
+  with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
-    const dim3 threads(threads_for(a.q.heads + a.k.heads, U));
-    if constexpr (sizeof(T) == 2) {
+    constexpr bool FULL = decltype(full)::value;
+    const int parts = parts_of(U, a.num_tokens, a.q.heads, a.k.heads, 0);
+    const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
+    if constexpr (sizeof(T) == 2 && FULL && U >= 8) {
       if (a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim)) {
-        hipLaunchKernelGGL((norm_rotary_kernel<T, U, NORM, false, true>), grid, threads, 0, stream, a);
+        hipLaunchKernelGGL((norm_rotary_kernel<T, U, FULL, NORM, false, true>), grid, threads, 0, stream, a, parts);
         return;
       }
     }
-    hipLaunchKernelGGL((norm_rotary_kernel<T, U, NORM, false, false>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((norm_rotary_kernel<T, U, FULL, NORM, false, false>), grid, threads, 0, stream, a, parts);
   });
 }
 
@@ -348,17 +490,21 @@ hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, hipStream_t st
 }
 
 hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream) {
-  const dim3 grid(min(a.num_tokens, kMaxGrid));
   const bool nt = a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim);
-  with_lanes(a.head_dim, [&](auto lanes) {
+  with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
-    if constexpr (U <= 8) {  // head_dim 64 and 128
-      const dim3 threads(threads_for(a.q.heads + 2 * a.k.heads, U));
-      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a); };
-      if (a.normed)
-        nt ? launch(norm_rotary_kernel<__bf16, U, true, true, true>) : launch(norm_rotary_kernel<__bf16, U, true, true, false>);
-      else
-        nt ? launch(norm_rotary_kernel<__bf16, U, false, true, true>) : launch(norm_rotary_kernel<__bf16, U, false, true, false>);
+    if constexpr (U <= 8 && decltype(full)::value) {  // head_dim 64 and 128
+      const int parts = parts_of(U, a.num_tokens, a.q.heads, a.k.heads, a.k.heads);
+      const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, parts); };
+      auto launch_kind = [&](auto normed) {
+        constexpr bool NORM = decltype(normed)::value;
+        if constexpr (U == 8) {
+          if (nt) return launch(norm_rotary_kernel<__bf16, U, true, NORM, true, true>);
+        }
+        launch(norm_rotary_kernel<__bf16, U, true, NORM, true, false>);
+      };
+      a.normed ? launch_kind(std::true_type()) : launch_kind(std::false_type());
     }
   });
   return hipGetLastError();
@@ -367,13 +513,14 @@ hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream
 hipError_t launch_norm_rotary_backward(const NormRotaryArgs& a, int dtype, hipStream_t stream) {
   const int groups = grad_groups(a.num_tokens);
   if (groups > 0)
-    with_lanes(a.head_dim, [&](auto lanes) {
+    with_lanes(a.head_dim, [&](auto lanes, auto full) {
       constexpr int U = decltype(lanes)::value;
-      const dim3 threads(threads_for(a.q.heads + a.k.heads, U));
+      constexpr bool FULL = decltype(full)::value;
+      const dim3 threads(kThreads);
       if (dtype == PDA_DTYPE_BF16)
-        hipLaunchKernelGGL((norm_rotary_grad_kernel<__bf16, U>), dim3(groups), threads, 0, stream, a);
+        hipLaunchKernelGGL((norm_rotary_grad_kernel<__bf16, U, FULL>), dim3(groups), threads, 0, stream, a);
       else
-        hipLaunchKernelGGL((norm_rotary_grad_kernel<float, U>), dim3(groups), threads, 0, stream, a);
+        hipLaunchKernelGGL((norm_rotary_grad_kernel<float, U, FULL>), dim3(groups), threads, 0, stream, a);
     });
   if (a.d_weight[0] || a.d_weight[1])
     hipLaunchKernelGGL(weight_grad_kernel, dim3(2 * a.head_dim / kSumColumns), dim3(kThreads), 0, stream, a.part, groups,

@@ -33,8 +33,9 @@ struct NormRotaryArgs {
   float* part;                // [grad_groups()][2][D]
 };
 
-// Workgroups of a backward pass; each leaves one partial sum of the weights' gradients.
-inline int grad_groups(int64_t num_tokens) { return (int)(num_tokens < 1024 ? num_tokens : 1024); }
+// Workgroups of a backward pass (4 wavefronts, a token each at a time); each leaves one
+// partial sum of the weights' gradients.
+inline int grad_groups(int64_t num_tokens) { return (int)(num_tokens < 4 * 768 ? (num_tokens + 3) / 4 : 768); }
 
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream);

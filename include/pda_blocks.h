@@ -70,7 +70,10 @@ typedef struct pda_token_rows {
 int pda_blocks_workspace_bytes(const pda_block_pool *pool, size_t *bytes);
 
 /* Resize every row for context_lens (device int32 [num_seqs]) and, with `rows` (may be
- * NULL), write the slot map of its rows.  `workspace`: any contents, 16-byte aligned. */
+ * NULL), write the slot map of its rows.  `workspace`: pda_blocks_workspace_bytes() bytes,
+ * 16-byte aligned, filled with ZEROS before its first use; a call leaves it ready for the
+ * next one (of any pool), and calls that overlap on the GPU need separate ones.
+ * context_lens, row_start, positions and slots overlap no buffer of the pool. */
 int pda_blocks_resize(const pda_block_pool *pool, const int32_t *context_lens, const pda_token_rows *rows,
                       void *workspace, size_t workspace_bytes, hipStream_t stream);
 

@@ -9,9 +9,13 @@
 // (read from its row, not from the stack, so nothing here waits for another
 // workgroup's store), else the old stack's place C - 1 - (x - F).
 //
-// One workgroup forms the sums and the new counts (plan_kernel); then a workgroup for every
-// kSpan entries of every row moves that row's ids and writes the slots of the tokens in those
-// blocks (move_kernel).
+// Up to kOneSeqs sequences it is one launch (resize_kernel): every workgroup forms all the sums,
+// a thread to a sequence, and takes its share of the ids and of the slot map; the last one to
+// have read the held counts writes the new ones.  For more, one workgroup forms the sums and
+// the new counts (plan_kernel); then a workgroup for every kSpan entries of every row moves
+// that row's ids and writes the slots of the tokens in those blocks (move_kernel).
+#include <algorithm>
+
 #include "pda_blocks_internal.h"
 
 namespace pda {
@@ -165,6 +169,177 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const BlocksArgs a) 
     for (int64_t r = start + threadIdx.x; r < end && r - start + first < 0; r += kMoveThreads) write_row(a, r, -1, -1);
 }
 
+// The whole resize, every workgroup with all the sums: the first workgroup moves up to kOwn of each
+// row's ids, a row to a thread; what is left is shared out a row to a wavefront, and the slot map
+// a token row to a thread.  An id is read from where it was before the call, so no workgroup reads
+// what another has written.  Two calls, us, against the two kernels: 256 sequences of up to 4096
+// tokens, 5 new ones each and back, 11.9 / 16.1 (of which 4.4 a call are the calls themselves);
+// all of their 33000 blocks granted and put back 17.4 / 16.1.  With one workgroup for everything the
+// first took 9.8 and the second 32.
+constexpr int kOneSeqs = kPlanThreads;
+constexpr int kOwn = 4;
+constexpr int64_t kEntriesEach = 8192, kRowsEach = 2048;  // of a workgroup
+// With more token rows than this the two kernels take over, whose threads need not find
+// their row's sequence.  Admitted and released in two calls, us, one launch each / two: 32000
+// rows of 8 sequences 14.5 / 19.0, 25600 of 256 16.4 / 16.6, 64000 of 64 16.1 / 16.7, 115200
+// of 128 18.7 / 16.9, 128000 of 256 16.6 / 16.4.
+constexpr int kOneRows = 65536;
+constexpr int64_t kMostGroups = 128;
+constexpr int kAhead = 4;  // entries of a row that a lane has in flight
+__global__ void __launch_bounds__(kPlanThreads) resize_kernel(const BlocksArgs a) {
+  const int group = blockIdx.x, groups = gridDim.x;
+  __shared__ int64_t sums[2][kPlanWaves];
+  __shared__ int most_granted[kPlanWaves];
+  __shared__ int back_at[kOneSeqs], need_of[kOneSeqs], held_of[kOneSeqs], grant_at[kOneSeqs], start_of[kOneSeqs + 1];
+  __shared__ bool last;
+  struct Rest {
+    int row, from, count, rank;  // count below 0: put back
+  };
+  __shared__ Rest rest[kOneSeqs];
+  __shared__ int rests[kPlanWaves];
+  const int B = a.pool.num_seqs, width = a.pool.max_blocks_per_seq, n = a.rows.num_rows;
+  const int b = threadIdx.x, lane = b % kWaveSize, wave = b / kWaveSize;
+  const bool mine = b < B;
+  const int held = mine ? clamp_to(a.pool.held[b], width) : 0;
+  const int need = mine ? blocks_for(a, a.lens[b]) : 0;
+  const int count = clamp_to(a.pool.counts[0], a.pool.num_blocks);
+  if (n > 0 && a.rows.row_start) {
+    if (b <= B) start_of[b] = clamp_to(a.rows.row_start[b], n);
+    if (b == 0) start_of[B] = clamp_to(a.rows.row_start[B], n);
+  }
+  // both sums at once
+  const int back = max(held - need, 0), want = max(need - held, 0);
+  int64_t x = back, y = want;
+#pragma unroll
+  for (int o = 1; o < kWaveSize; o <<= 1) {
+    const int64_t p = __shfl_up(x, o), q = __shfl_up(y, o);
+    if (lane >= o) x += p, y += q;
+  }
+  if (lane == kWaveSize - 1) sums[0][wave] = x, sums[1][wave] = y;
+  __syncthreads();
+  int64_t all_back = 0, all_want = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) x += sums[0][w], y += sums[1][w];
+    all_back += sums[0][w], all_want += sums[1][w];
+  }
+  const int stack = (int)min<int64_t>(count + all_back, a.pool.num_blocks), put = stack - count;
+  const bool fits = y <= stack;
+  const int first_back = (int)min<int64_t>(x - back, a.pool.num_blocks), first_grant = fits ? (int)(y - want) : 0;
+  const int held_new = need <= held || fits ? need : held;
+  back_at[b] = mine ? first_back : 0x7fffffff, need_of[b] = need, held_of[b] = held;
+  grant_at[b] = want > 0 && fits ? first_grant : -1;
+  int g = fits ? (int)y : 0;  // (sums do not fall: the largest that fits is all that is granted)
+#pragma unroll
+  for (int o = 1; o < kWaveSize; o <<= 1) g = max(g, __shfl_xor(g, o));
+  if (lane == 0) most_granted[wave] = g;
+  __syncthreads();
+  if (groups > 1 && b == 0) last = __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
+  if (groups > 1) __syncthreads();
+  if (groups == 1 || last) {  // every workgroup has read the counts (its sums are formed)
+    if (mine) a.pool.held[b] = held_new;
+    if (b == 0) {
+#pragma unroll
+      for (int w = 0; w < kPlanWaves; ++w) g = max(g, most_granted[w]);
+      a.pool.counts[0] = stack - g;
+      a.pool.counts[1] = (int)min<int64_t>(max<int64_t>(all_want - stack, 0), 0x7fffffff);
+      if (groups > 1) *a.arrived = 0;  // for the next call
+    }
+  }
+  // A row's moves: entries from, from + 1, ... (`grant`: granted, otherwise put back), of these ranks on.
+  struct Moves {
+    int row, from, count, rank;
+    bool grant;
+  };
+  auto source = [&](const Moves& m, int e) -> const int32_t* {
+    if (!m.grant) return a.pool.block_table + (size_t)m.row * width + m.from + e;
+    const int r = m.rank + e;
+    if (r >= put) return a.pool.free_blocks + clamp_to(count - 1 - (r - put), a.pool.num_blocks - 1);
+    int lo = 0, hi = B - 1;  // an entry put back in this call: the last row whose ranks begin at or below it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (back_at[mid] <= r)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return a.pool.block_table + (size_t)lo * width + clamp_to(need_of[lo] + r - back_at[lo], width - 1);
+  };
+  auto store = [&](const Moves& m, int e, int id) {
+    if (m.grant)
+      a.pool.block_table[(size_t)m.row * width + m.from + e] = id;
+    else if (m.rank + e < put)
+      a.pool.free_blocks[clamp_to(stack - 1 - (m.rank + e), a.pool.num_blocks - 1)] = id;
+  };
+  const bool grows = want > 0 && fits;
+  const Moves my{b, grows ? held : need, grows ? want : back, grows ? first_grant : first_back, grows};
+  const int own = group == 0 ? min(my.count, kOwn) : 0;
+  int ids[kOwn];
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e)
+    if (e < own) ids[e] = *source(my, e);
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e)
+    if (e < own) store(my, e, ids[e]);
+  const bool more = my.count > kOwn;
+  const uint64_t mask = __builtin_amdgcn_ballot_w64(more);
+  if (lane == 0) rests[wave] = __builtin_popcountll(mask);
+  __syncthreads();
+  int place = __builtin_popcountll(mask & ((1ull << lane) - 1)), all_rests = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) place += w < wave ? rests[w] : 0, all_rests += rests[w];
+  if (all_rests > 0) {  // (the same for all threads)
+    if (more) rest[place] = Rest{b, my.from, grows ? my.count : -my.count, my.rank};
+    __syncthreads();
+    for (int i = group * kPlanWaves + wave; i < all_rests; i += groups * kPlanWaves) {
+      const Rest x = rest[i];
+      const Moves m{x.row, x.from, abs(x.count), x.rank, x.count > 0};
+      for (int e0 = kOwn + lane; e0 < m.count; e0 += kAhead * kWaveSize) {
+        int id[kAhead];
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h)
+          if (e0 + h * kWaveSize < m.count) id[h] = *source(m, e0 + h * kWaveSize);
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h)
+          if (e0 + h * kWaveSize < m.count) store(m, e0 + h * kWaveSize, id[h]);
+      }
+    }
+  }
+  // the slot map
+  for (int64_t r = (int64_t)group * kPlanThreads + b; r < n; r += (int64_t)groups * kPlanThreads) {
+    int row;
+    int64_t t;
+    if (a.rows.row_start) {
+      int lo = 0, hi = B - 1;  // the last row that starts at or before r
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start_of[mid] <= r)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      row = r >= start_of[lo] && r < start_of[lo + 1] ? lo : -1;
+      t = r - start_of[lo + 1];
+    } else {
+      row = (int)r / a.uniform_rows;
+      t = r - (int64_t)(row + 1) * a.uniform_rows;
+    }
+    if (row >= 0) t += (int)min<int64_t>(max(a.lens[row], 0), (int64_t)kBlockTokens * width);
+    if (row < 0 || t < 0) {
+      write_row(a, r, -1, -1);
+      continue;
+    }
+    const int j = (int)(t / kBlockTokens);
+    const int32_t* at = nullptr;  // where the block's id was before the call
+    if (j < min(held_of[row], need_of[row]))
+      at = a.pool.block_table + (size_t)row * width + j;
+    else if (grant_at[row] >= 0 && j < need_of[row])
+      at = source(Moves{row, held_of[row], 0, grant_at[row], true}, j - held_of[row]);
+    const int id = at ? *at : -1;
+    write_row(a, r, (int)t, (unsigned)id < (unsigned)a.pool.num_blocks ? id * kBlockTokens + (int)(t % kBlockTokens) : -1);
+  }
+}
+
 template <bool MOVE>
 hipError_t launch_moves(const BlocksArgs& a, hipStream_t stream) {
   const unsigned spans = (unsigned)((a.pool.max_blocks_per_seq + kSpan - 1) / kSpan);
@@ -176,6 +351,12 @@ hipError_t launch_moves(const BlocksArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_blocks_resize(const BlocksArgs& a, hipStream_t stream) {
+  if (a.pool.num_seqs <= kOneSeqs && a.rows.num_rows <= kOneRows) {
+    const int64_t entries = (int64_t)a.pool.num_seqs * a.pool.max_blocks_per_seq;
+    const int64_t groups = std::max((entries + kEntriesEach - 1) / kEntriesEach, (a.rows.num_rows + kRowsEach - 1) / kRowsEach);
+    hipLaunchKernelGGL(resize_kernel, dim3((unsigned)std::min(groups, kMostGroups)), dim3(kPlanThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? launch_moves<true>(a, stream) : e;

@@ -33,7 +33,7 @@ int check_rows(const pda_token_rows* rows, int32_t num_seqs, pda::BlocksArgs* a)
 }
 
 size_t workspace_of(int32_t num_seqs) {
-  return num_seqs == 0 ? 0 : 2 * sizeof(int32_t) + (size_t)num_seqs * sizeof(pda::BlockMove);
+  return num_seqs == 0 ? 0 : 4 * sizeof(int32_t) + (size_t)num_seqs * sizeof(pda::BlockMove);
 }
 
 }  // namespace
@@ -69,7 +69,8 @@ int pda_blocks_resize(const pda_block_pool* pool, const int32_t* context_lens, c
   a.pool = *pool;
   a.lens = context_lens;
   a.table = pool->block_table;
-  a.totals = static_cast<int32_t*>(workspace);
+  a.arrived = static_cast<int32_t*>(workspace);
+  a.totals = a.arrived + 2;
   a.moves = reinterpret_cast<pda::BlockMove*>(a.totals + 2);
   const hipError_t e = pool->num_seqs > 0 ? pda::launch_blocks_resize(a, stream) : pda::launch_slot_map(a, stream);
   return e == hipSuccess ? PDA_OK : PDA_ERR_HIP;
@@ -91,7 +92,7 @@ int pda_slot_map(int32_t num_seqs, int32_t num_blocks, int32_t max_blocks_per_se
   a.lens = context_lens;
   a.table = block_table;
   a.moves = nullptr;
-  a.totals = nullptr;
+  a.totals = a.arrived = nullptr;
   return pda::launch_slot_map(a, stream) == hipSuccess ? PDA_OK : PDA_ERR_HIP;
 }
 

@@ -20,6 +20,7 @@ struct BlocksArgs {
   const int32_t* table;  // (of the pool, or the slot map's own)
   pda_token_rows rows;
   int32_t uniform_rows;  // rows per sequence where row_start is null
+  int32_t* arrived;      // (workspace) workgroups that have read the held counts; 0 between calls
   BlockMove* moves;      // [num_seqs] (workspace)
   int32_t* totals;       // [2] (workspace): free blocks before, blocks put back
 };

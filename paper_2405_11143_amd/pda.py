@@ -1482,8 +1482,11 @@ def bind_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, posit
     """pda_blocks_resize bound to a pool (make_block_pool), lengths int32 [num_seqs] and the given
     (else the current) stream: every row grown or shrunk to hold its length.  With positions
     and/or slots (int32 [num_rows]) the slot map of the new tokens is written to them: row_start int32
-    [num_seqs + 1] says whose they are, None: the same number of every sequence.  Calling it returns
+    [num_seqs + 1] says whose they are, None: the same number of every sequence.  `workspace`: uint8 zeros
+    of pda_blocks_workspace_bytes, allocated here when not given.  Calling it returns
     (block_table, positions, slots)."""
+    import torch
+
     _check_lens(context_lens, pool.num_seqs)
     rows, tensors = _token_map(pool.num_seqs, row_start, positions, slots)
     device = _same_device(*pool.tensors, context_lens, workspace, *tensors)
@@ -1491,6 +1494,8 @@ def bind_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, posit
     rc = load_library().pda_blocks_workspace_bytes(ctypes.byref(pool), ctypes.byref(ws))
     if rc != PDA_OK:
         raise PdaError(rc, "pda_blocks_workspace_bytes")
+    if workspace is None and ws.value > 0:
+        workspace = _zeros_like(_empty((ws.value,), torch.uint8, device, stream, result=False), stream)
     workspace, ws_ptr, ws_bytes = _given_workspace(workspace, ws.value, device, stream)
     args = (ctypes.byref(pool), context_lens.data_ptr(), ctypes.byref(rows) if rows is not None else None, ws_ptr,
             ws_bytes, _stream_handle(stream, device))

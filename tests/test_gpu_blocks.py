@@ -82,7 +82,7 @@ def test_lengths_are_clamped(lens):
     np.testing.assert_array_equal(pos.cpu().numpy(), model.slot_map(np.clip(lens, 0, 160), np.arange(4) * 4, 12)[0])
 
 
-@pytest.mark.parametrize("B,n", [(1, 1), (5, 1), (4, 33), (2, 5000)])
+@pytest.mark.parametrize("B,n", [(1, 1), (5, 1), (4, 33), (2, 5000), (3, 30000)])
 def test_uniform_rows(B, n):
     """Without row_start every sequence has the same number of rows: positions in front of a short
     context are padding."""
@@ -141,3 +141,17 @@ def test_captured_and_replayed():
         model.resize(new)
         check_pool(pool, model)
         np.testing.assert_array_equal(slots.cpu().numpy(), model.slot_map(new, np.arange(10), 9)[1])
+
+
+def test_one_workspace_for_several_pools():
+    """A workspace of zeros serves one call after the other, on pools of different sizes and both ways of
+    running."""
+    rng = np.random.RandomState(8)
+    pools = [(pda.new_block_pool(B, 4000, width), Pool(B, 4000, width)) for B, width in ((1100, 300), (40, 700), (3, 8))]
+    workspace = torch.zeros(32768, dtype=torch.uint8, device="cuda")
+    for step in range(3):
+        for pool, model in pools:
+            lens = rng.randint(0, 100, len(model.held))
+            pda.pda_blocks_resize(pool, i32(lens), workspace=workspace)
+            model.resize(lens)
+            check_pool(pool, model)

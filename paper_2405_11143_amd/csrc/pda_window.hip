@@ -89,10 +89,9 @@ struct WindowFold {
     return ((x & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
   }
 
-  // The block's product where tokens that only some rows see hold infinities or NaN: those
-  // elements are left out, and counted for the rows that do see them, which become NaN there.
-  static __device__ __forceinline__ void product_apart(WT (&w)[TILES], const typename WT::Parts (&f)[TILES],
-                                                       const uint4 (&vr)[4], int tok0, const Limits& lim) {
+  // Tokens that only some rows see hold infinities or NaN: the rows that do see them become NaN in those
+  // columns (counted by a product of ones), and the elements are zeroed for the others.
+  static __device__ __forceinline__ void set_apart(WT (&w)[TILES], uint4 (&vr)[4], int tok0, const Limits& lim) {
     constexpr unsigned kOnes = 0x3f803f80u;
     unsigned partly[2] = {0u, 0u}, seen[TILES][2];  // of a fragment's two dwords: tokens 4 kg .. 4 kg + 3
 #pragma unroll
@@ -109,20 +108,22 @@ struct WindowFold {
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       const uint2 u = __builtin_bit_cast(uint2, v_part(w[0], vr, t));
-      const uint2 odd = make_uint2(odd_halves(u.x) & partly[0], odd_halves(u.y) & partly[1]);
-      const shortx4_t a = __builtin_bit_cast(shortx4_t, make_uint2(u.x & ~odd.x, u.y & ~odd.y));
-      const shortx4_t ones = __builtin_bit_cast(shortx4_t, make_uint2(odd.x & kOnes, odd.y & kOnes));
+      const shortx4_t ones = __builtin_bit_cast(
+          shortx4_t, make_uint2(odd_halves(u.x) & partly[0] & kOnes, odd_halves(u.y) & partly[1] & kOnes));
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
         const floatx4_t zero = {0.f, 0.f, 0.f, 0.f};
         const floatx4_t count = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
             ones, __builtin_bit_cast(shortx4_t, make_uint2(seen[x][0], seen[x][1])), zero, 0, 0, 0);
 #pragma unroll
-        for (int part = 0; part < 3; ++part)
-          w[x].o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, f[x].part[part], w[x].o[t], 0, 0, 0);
-#pragma unroll
         for (int e = 0; e < 4; ++e) w[x].o[t][e] = count[e] > 0.f ? __builtin_nanf("") : w[x].o[t][e];
       }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (lim.all(tok0 + 4 * w[0].kg + e)) continue;
+      vr[e].x &= ~odd_halves(vr[e].x), vr[e].y &= ~odd_halves(vr[e].y);
+      vr[e].z &= ~odd_halves(vr[e].z), vr[e].w &= ~odd_halves(vr[e].w);
     }
   }
 
@@ -147,10 +148,7 @@ struct WindowFold {
         if (!lim.some(t)) vr[e] = make_uint4(0u, 0u, 0u, 0u);  // nobody sees it: whatever it holds
         odd |= MULTI && !lim.all(t) && (odd_halves(vr[e].x) | odd_halves(vr[e].y) | odd_halves(vr[e].z) | odd_halves(vr[e].w)) != 0;
       }
-      if (MULTI && __builtin_amdgcn_ballot_w64(odd) != 0) {
-        product_apart(w, f, vr, tok0, lim);
-        return;
-      }
+      if (MULTI && __builtin_amdgcn_ballot_w64(odd) != 0) set_apart(w, vr, tok0, lim);
     }
 #pragma unroll
     for (int t = 0; t < VT; ++t) {

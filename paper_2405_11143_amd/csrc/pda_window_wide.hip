@@ -71,9 +71,6 @@ window_wide_kernel(const WindowArgs a) {
   const int up_min = L - n + 1 + t0, up_max = L - n + t1;
   const int low_min = window_start(up_min, a.window), low_max = window_start(up_max, a.window);
   const int sinks = a.sinks;
-  auto sees = [&](int t) { return t < up && (t < sinks || t >= low); };
-  auto all_see = [&](int t) { return t < up_min && (t < sinks || t >= low_max); };
-  auto some_see = [&](int t) { return t < up_max && (t < sinks || t >= low_min); };
   auto whole = [&](int t) { return t + kStep <= up_min && (t + kStep <= sinks || t >= low_max); };
   auto wanted = [&](int t) { return active && t < up_max && (t < sinks || t + kStep > low_min); };
 
@@ -140,13 +137,17 @@ window_wide_kernel(const WindowArgs a) {
 
   f32x16_t s;  // scores of the step to fold: reg i is token tok0 + 8 (i / 4) + 4 hh + i % 4
   float top;   // the largest of them
-  auto scores = [&](const uint4* blocks) {
+  auto k_frags = [&](const uint4* blocks, uint4(&kf)[KS]) {
+#pragma unroll
+    for (int c = 0; c < KS; ++c) kf[c] = blocks[k_piece + 32 * c];
+  };
+  auto scores = [&](const uint4(&kf)[KS]) {
     f32x16_t x;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
     for (int c = 0; c < KS; ++c)
-      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, blocks[k_piece + 32 * c]), q[c], x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[c]), q[c], x, 0, 0, 0);
     return x;
   };
   auto largest = [&] {
@@ -156,12 +157,18 @@ window_wide_kernel(const WindowArgs a) {
     top = max3(x, s[15], s[15]);
     asm volatile("" : "+v"(top));  // the MFMA results are first read in their own basic block
   };
+  // The first x of 32 bits (all, or none).
+  auto first_bits = [](int x) { return x >= 32 ? 0xffffffffu : (1u << max(x, 0)) - 1u; };
   auto mask = [&](int tok0) {
     if (!whole(tok0)) {  // wavefront-uniform: some row does not see some of these tokens
       asm volatile("");  // a branch: as selects the masking would run on every step
+      const int base = tok0 + 4 * hh;  // a bit for every token that the lane's row sees, then two instructions a score
+      const unsigned seen = first_bits(up - base) & (first_bits(sinks - base) | ~first_bits(low - base));
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!sees(tok0 + 4 * hh + 8 * (i / 4) + i % 4)) s[i] = -__builtin_huge_valf();
+      for (int i = 0; i < 16; ++i) {
+        const unsigned m = (unsigned)__builtin_amdgcn_sbfe((int)seen, 8 * (i / 4) + i % 4, 1);
+        s[i] = __uint_as_float((__float_as_uint(s[i]) & m) | (0xff800000u & ~m));
+      }
       largest();
     }
   };
@@ -183,56 +190,70 @@ window_wide_kernel(const WindowArgs a) {
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int t = 0; t < VT; ++t) vf[m][t] = v_frag(m, t);
+    uint4 kf[KS];  // read here, not where they are used: the products would wait for each in turn
+    k_frags(next_blocks, kf);
+    __builtin_amdgcn_sched_barrier(0);
+    // Where every element is finite, a token's probability of 0 leaves it out of a row that does not see it.
+    bool odd = false;
     if (!whole(tok0)) {  // wavefront-uniform
       asm volatile("");
-      // Fragment words: tokens 4 hh + 16 m + {0, 2, 8, 10}, and the one after.  V rows that no row
-      // sees are zeroed, whatever they hold.  Infinities and NaN of tokens that only some rows see are left
-      // out, and counted for the rows that do see them, which become NaN there.
-      unsigned some[2][4], partly[2][4], mine[2][4];
+      typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+      u16x2_t top16 = {0, 0};
+      auto word = [&](unsigned x) { top16 = __builtin_elementwise_max(top16, __builtin_bit_cast(u16x2_t, x & 0x7fff7fffu)); };
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) word(vf[m][t].x), word(vf[m][t].y), word(vf[m][t].z), word(vf[m][t].w);
+      odd = top16[0] >= 0x7f80 || top16[1] >= 0x7f80;
+    }
+    int any = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_ballot_w64(odd) != 0 ? 1 : 0);
+    if (any) {
+      // Infinities and NaN of tokens that only some rows see are left out of the product, and make the
+      // rows that do see them NaN there, a token at a time (v - v is 0 for the others).
+#pragma unroll 1
+      for (int x = 0; x < kStep; ++x) {
+        const int t = tok0 + x;
+        if (!(t < up_max && (t < sinks || t >= low_min)) || (t < up_min && (t < sinks || t >= low_max))) continue;
+        const bool mine = t < up && (t < sinks || t >= low);
+        const int perm = D == 128 ? 4 * (x & 3) : 4 * ((x >> 1) & 1);
+        const uint2* row = reinterpret_cast<const uint2*>(blocks + (x / 16) * S::kBlockPieces + S::kTilePieces + (x % 16) * RP);
+#pragma unroll
+        for (int u = 0; u < VT; ++u)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint2 v = row[2 * ((4 * u + k) ^ perm) + hh];  // columns 32 u + 8 k + 4 hh .. + 3
+            const float vv[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                                 __uint_as_float(v.y & 0xffff0000u)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u][4 * k + e] = mine ? o[u][4 * k + e] + (vv[e] - vv[e]) : o[u][4 * k + e];
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      }
+    }
+    asm volatile("" ::: "memory");  // (two branches of their own: as one they spilled 76 bytes a lane)
+    any = __builtin_amdgcn_readfirstlane(any);
+    if (any) {
+      // (V rows that no row of the tile sees are zeroed)
+      const int base = tok0 + 4 * hh;
+      auto bits = [&](int u, int l) { return first_bits(u - base) & (first_bits(sinks - base) | ~first_bits(l - base)); };
+      const unsigned some = bits(up_max, low_min), every = bits(up_min, low_max);
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          some[m][h] = partly[m][h] = mine[m][h] = 0u;
+          // word h of fragment m: tokens 16 m + {0, 2, 8, 10} + 4 hh, and the ones after
+          const int c = 16 * m + 8 * (h / 2) + 2 * (h % 2);
+          auto halves = [&](unsigned b) {
+            return ((unsigned)__builtin_amdgcn_sbfe((int)b, c, 1) & 0x0000ffffu) |
+                   ((unsigned)__builtin_amdgcn_sbfe((int)b, c + 1, 1) & 0xffff0000u);
+          };
+          const unsigned seen = halves(some), by_all = halves(every);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int t = tok0 + 4 * hh + 16 * m + 8 * (h / 2) + 2 * (h % 2) + e;
-            const unsigned half = e ? 0xffff0000u : 0x0000ffffu;
-            some[m][h] |= some_see(t) ? half : 0u;
-            partly[m][h] |= some_see(t) && !all_see(t) ? half : 0u;
-            mine[m][h] |= sees(t) ? half & 0x3f803f80u : 0u;
+          for (int t = 0; t < VT; ++t) {
+            unsigned& v = h == 0 ? vf[m][t].x : h == 1 ? vf[m][t].y : h == 2 ? vf[m][t].z : vf[m][t].w;
+            v &= seen & (by_all | ~odd_halves(v));
           }
         }
-      bool odd = false;
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          vf[m][t].x &= some[m][0], vf[m][t].y &= some[m][1], vf[m][t].z &= some[m][2], vf[m][t].w &= some[m][3];
-          odd |= ((odd_halves(vf[m][t].x) & partly[m][0]) | (odd_halves(vf[m][t].y) & partly[m][1]) |
-                  (odd_halves(vf[m][t].z) & partly[m][2]) | (odd_halves(vf[m][t].w) & partly[m][3])) != 0;
-        }
-      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          f32x16_t count;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) count[i] = 0.f;
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            uint4& v = vf[m][t];
-            const uint4 out = make_uint4(odd_halves(v.x) & partly[m][0], odd_halves(v.y) & partly[m][1],
-                                         odd_halves(v.z) & partly[m][2], odd_halves(v.w) & partly[m][3]);
-            v = make_uint4(v.x & ~out.x, v.y & ~out.y, v.z & ~out.z, v.w & ~out.w);
-            constexpr unsigned kOnes = 0x3f803f80u;
-            count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8_t, make_uint4(out.x & kOnes, out.y & kOnes, out.z & kOnes, out.w & kOnes)),
-                __builtin_bit_cast(bf16x8_t, make_uint4(mine[m][0], mine[m][1], mine[m][2], mine[m][3])), count, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
-        }
-      }
     }
     float ref = m_run;
     if (__builtin_amdgcn_ballot_w64(fmaf(top, scale, -m_run) > 8.f || fabsf(m_run) > kExactMax) != 0) {
@@ -247,7 +268,7 @@ window_wide_kernel(const WindowArgs a) {
 #pragma unroll
       for (int t = 0; t < VT; ++t) o[t] *= al;
     }
-    const f32x16_t ns = scores(next_blocks);
+    const f32x16_t ns = scores(kf);
     bf16x8_t bh[2], bl[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -257,12 +278,12 @@ window_wide_kernel(const WindowArgs a) {
       l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
       unsigned hw[4], lw[4];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const unsigned h0 = __float_as_uint(pr[2 * h]) & 0xffff0000u;
-        const unsigned h1 = __float_as_uint(pr[2 * h + 1]) & 0xffff0000u;
-        hw[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
+      for (int h = 0; h < 4; ++h) {  // rounded to nearest, and what is left of it: half the error of cutting off
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-        const bf16x2_t l2 = {(__bf16)(pr[2 * h] - __uint_as_float(h0)), (__bf16)(pr[2 * h + 1] - __uint_as_float(h1))};
+        const bf16x2_t h2 = {(__bf16)pr[2 * h], (__bf16)pr[2 * h + 1]};
+        hw[h] = __builtin_bit_cast(unsigned, h2);
+        const bf16x2_t l2 = {(__bf16)(pr[2 * h] - __uint_as_float(hw[h] << 16)),
+                             (__bf16)(pr[2 * h + 1] - __uint_as_float(hw[h] & 0xffff0000u))};
         lw[h] = __builtin_bit_cast(unsigned, l2);
       }
       bh[m] = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
@@ -313,7 +334,9 @@ window_wide_kernel(const WindowArgs a) {
         continue;
       }
       if (!ready) {
-        s = scores(st.buf[step % kBuffers][0]);
+        uint4 kf[KS];
+        k_frags(st.buf[step % kBuffers][0], kf);
+        s = scores(kf);
         largest();
         mask(tok0);
       }

@@ -317,28 +317,37 @@ __global__ void __launch_bounds__(kMergeRows * kWaveSize) window_merge_kernel(co
   const int lane = threadIdx.x & (kWaveSize - 1);
   if ((size_t)row >= (size_t)s.num_seqs * s.num_query_tokens * s.num_q_heads) return;
   const int i = (row / s.num_q_heads) % s.num_query_tokens, b = row / (s.num_q_heads * s.num_query_tokens);
-  int L = s.lens[b];
-  L = L < 0 ? 0 : (L > s.max_context_len ? s.max_context_len : L);
-  const int parts = window_partitions(a, L, i / a.group_tokens);
-  if (parts <= 1) return;  // pass 1 wrote the row
   const size_t first = (size_t)row * s.slots_per_row;
-  constexpr float kNone = -__builtin_huge_valf();
-  float M = kNone;
-  for (int x = lane; x < parts; x += kWaveSize) M = fmaxf(M, s.part_m[first + x]);
-#pragma unroll
-  for (int o = 1; o < kWaveSize; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-  float lsum = 0.f, acc[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = 0.f;
-  for (int x0 = 0; x0 < parts; x0 += kMergeAhead) {
-    float m[kMergeAhead], l[kMergeAhead], v[kMergeAhead][C];
+  // The first slots are loaded before it is known how many the row has: the rest is one chain of
+  // latencies less.
+  float m[kMergeAhead], l[kMergeAhead], v[kMergeAhead][C];
+  auto load = [&](int x0, int count) {
 #pragma unroll
     for (int x = 0; x < kMergeAhead; ++x) {
-      const size_t slot = first + min(x0 + x, parts - 1);
+      const size_t slot = first + min(x0 + x, count - 1);
       m[x] = s.part_m[slot], l[x] = s.part_l[slot];
 #pragma unroll
       for (int c = 0; c < C; ++c) v[x][c] = s.part_o[slot * D + lane * C + c];
     }
+  };
+  load(0, s.slots_per_row);
+  int L = s.lens[b];
+  L = L < 0 ? 0 : (L > s.max_context_len ? s.max_context_len : L);
+  const int parts = window_partitions(a, L, i / a.group_tokens);
+  if (parts <= 1) return;  // pass 1 wrote the row
+  float M = -__builtin_huge_valf();
+#pragma unroll
+  for (int x = 0; x < kMergeAhead; ++x) M = x < parts ? fmaxf(M, m[x]) : M;
+  if (parts > kMergeAhead) {
+    for (int x = kMergeAhead + lane; x < parts; x += kWaveSize) M = fmaxf(M, s.part_m[first + x]);
+#pragma unroll
+    for (int o = 1; o < kWaveSize; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+  }
+  float lsum = 0.f, acc[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) acc[c] = 0.f;
+  for (int x0 = 0; x0 < parts; x0 += kMergeAhead) {
+    if (x0 > 0) load(x0, parts);
 #pragma unroll
     for (int x = 0; x < kMergeAhead; ++x) {
       if (x0 + x >= parts) break;

@@ -12,6 +12,18 @@ namespace {
 
 constexpr int64_t kMostItems = (1 << 24) - 1;        // workgroups of 256: a launch has less than 2^32 threads
 constexpr int64_t kMostMergeRows = 4 * kMostItems;   // the merge: workgroups of 256 for 4 rows
+// Narrow items are split into as many as make one for every compute unit, of at least
+// kNarrowLeast tokens, where that shortens an item by kNarrowGain.  Wide ones into up to two for
+// every unit, of at least kWideLeast tokens, or one for every unit of at least kWideFew;
+// two from one would share a unit that one has to itself.  Decode steps of 32 / 8 heads of
+// 128, us, this rule / whole / the best of partitions of 128 to 2064: 1 sequence with a window of 512 7.9
+// / 7.9 / 9.3, of 1024 10.3 / 12.9 / 10.4, of 4096 13.1 / - / 12.7; 4: 8.9 / 8.9 / 10.1, 11.2 /
+// 13.5 / 11.1, 17.9 / - / 18.0; 8: 9.2 / 9.2 / 10.7, 12.8 / 14.1 / 13.0, 26.9 / - / 27.0; 16 of 1024
+// 15.7 / 15.7 / 17.7, of 4096 45.8 / - / 46.0.  64 new tokens over a window of 1024: 1 sequence whole
+// 44.8, in 288s 24.6, in 128s 21.9; 4 45.7, 30.3, 41.7; 8 47.2, 43.1, 66.8; 512 new ones of 2
+// (256 items) 51.0 whole, 68.5 in 512s.
+constexpr int64_t kNarrowAtOnce = 256, kNarrowLeast = 176, kNarrowGain = 600;
+constexpr int64_t kWideAtOnce = 512, kWideLeast = 256, kWideFew = 128, kWideGain = 400;
 
 bool aligned(const void* ptr, size_t a) { return ((uintptr_t)ptr % a) == 0; }
 
@@ -34,6 +46,24 @@ int64_t longest_list(const pda_problem* p, const pda_window* w, const Plan& plan
   return std::min(whole, apart) * u;
 }
 
+// Tokens per partition when the caller leaves them to the library.  Lists are as long as
+// the window wherever contexts are longer, so there is nothing to balance, and splitting pays only
+// where it fills compute units that would be idle, by more than the merge costs.
+int64_t partition_rule(const pda_problem* p, const Plan& plan, int64_t len) {
+  const int64_t units = (int64_t)p->num_seqs * p->num_kv_heads * plan.num_groups;
+  if (units == 0) return len;
+  int64_t pieces, gain;
+  if (plan.unit == pda::kWindowUnit) {
+    pieces = std::min(kNarrowAtOnce / units, len / kNarrowLeast);
+    gain = kNarrowGain;
+  } else {
+    const int64_t room = kWideAtOnce / units;
+    pieces = room < 3 ? 1 : std::min(room, std::max(len / kWideLeast, std::min(room / 2, len / kWideFew)));
+    gain = kWideGain;
+  }
+  return pieces < 2 || len - len / pieces < gain ? len : (len + pieces - 1) / pieces;
+}
+
 int make_plan(const pda_problem* p, const pda_window* w, Plan* plan) {
   if (!w) return PDA_ERR_NULL;
   int rc = pda_plan(p, &plan->info);
@@ -46,12 +76,8 @@ int make_plan(const pda_problem* p, const pda_window* w, Plan* plan) {
   plan->group_tokens = narrow ? n : std::min(n, plan->query_chunk * (pda::kWindowWideRows / pda::kMaxGroup));
   plan->num_groups = (n + plan->group_tokens - 1) / plan->group_tokens;
   const int64_t len = longest_list(p, w, *plan);
-  // the partitions of pda_decode's plan for contexts as long as what is read here
-  pda_problem like = *p;
-  like.max_context_len = (int32_t)std::min<int64_t>(len, p->max_context_len);
-  rc = pda_plan(&like, &plan->info);
-  if (rc != PDA_OK) return rc;
-  int64_t tokens = (plan->info.partition_tokens + plan->unit - 1) / plan->unit * plan->unit;
+  int64_t tokens = p->partition_tokens > 0 ? p->partition_tokens : partition_rule(p, *plan, len);
+  tokens = std::max<int64_t>(plan->unit, (std::min(tokens, len) + plan->unit - 1) / plan->unit * plan->unit);
   const int64_t parts = std::max<int64_t>(1, (len + tokens - 1) / tokens);
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
   const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads;

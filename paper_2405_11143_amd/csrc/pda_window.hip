@@ -194,7 +194,7 @@ window_kernel(const WindowArgs a) {
   const int rows = n * G;
   int L = s.lens[b];
   L = L < 0 ? 0 : (L > s.max_context_len ? s.max_context_len : L);
-  const WindowSpan span = window_span(L, n, 0, n, a.window, a.sinks, kWindowUnit);
+  const WindowSpan span = window_span(L, n, 0, n, a.window, a.sinks);
   const int per_part = s.partition_tokens / kWindowUnit;
   const int parts = (span.count() + per_part - 1) / per_part;
   auto out_row = [&](int r) {  // output row of the item's row r (token-major, then the G heads)
@@ -232,12 +232,12 @@ window_kernel(const WindowArgs a) {
   uint4 ka[WT::NC], va[4], kb[WT::NC], vb[4];
   for (int c0 = v0; c0 < v1; c0 += kWaveSize) {
     const int cn = min(kWaveSize, v1 - c0);
-    const int ids = lane < cn ? table_row[span.token(c0 + lane, 1)] : 0;
+    const int ids = lane < cn ? table_row[span.block(c0 + lane)] : 0;
     auto load = [&](uint4(&k)[WT::NC], uint4(&v)[4], int i) {
       w[0].load_tiles(k, v, kpool, vpool, block_bytes, s.num_blocks, __builtin_amdgcn_readlane(ids, min(i, cn - 1)), i < cn);
     };
     auto fold = [&](const uint4(&k)[WT::NC], uint4(&v)[4], int i) {
-      Fold::block(w, k, v, span.token(c0 + i, kWindowUnit), lim);
+      Fold::block(w, k, v, span.token(c0 + i), lim);
     };
     load(ka, va, 0);
     for (int i = 0; i < cn; i += 2) {

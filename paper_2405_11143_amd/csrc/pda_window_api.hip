@@ -31,17 +31,18 @@ int query_tokens(const pda_problem* p) { return p->num_query_tokens > 0 ? p->num
 
 struct Plan {
   pda_plan_info info;
-  int unit, group_tokens, num_groups, query_chunk;
+  bool narrow;
+  int group_tokens, num_groups, query_chunk;
   int64_t items;
   size_t slots;  // partial states, 0 when nothing is split
 };
 
 // The most tokens that a work item's list holds.
 int64_t longest_list(const pda_problem* p, const pda_window* w, const Plan& plan) {
-  const int64_t u = plan.unit;
+  constexpr int64_t u = pda::kWindowUnit;
   auto units = [&](int64_t tokens) { return (tokens + u - 1) / u; };
   const int64_t whole = units(p->max_context_len);
-  // (a window starts anywhere in its first unit)
+  // (a window starts anywhere in its first block)
   const int64_t apart = units(w->num_sinks) + units((int64_t)w->window + plan.group_tokens - 1) + 1;
   return std::min(whole, apart) * u;
 }
@@ -53,7 +54,7 @@ int64_t partition_rule(const pda_problem* p, const Plan& plan, int64_t len) {
   const int64_t units = (int64_t)p->num_seqs * p->num_kv_heads * plan.num_groups;
   if (units == 0) return len;
   int64_t pieces, gain;
-  if (plan.unit == pda::kWindowUnit) {
+  if (plan.narrow) {
     pieces = std::min(kNarrowAtOnce / units, len / kNarrowLeast);
     gain = kNarrowGain;
   } else {
@@ -71,13 +72,13 @@ int make_plan(const pda_problem* p, const pda_window* w, Plan* plan) {
   if (w->window < 1 || w->num_sinks < 0) return PDA_ERR_SHAPE;
   const int n = query_tokens(p), G = p->num_q_heads / p->num_kv_heads;
   plan->query_chunk = std::min(n, pda::kMaxGroup / G);
-  const bool narrow = (int64_t)n * G <= pda::kWindowNarrowRows;
-  plan->unit = narrow ? pda::kWindowUnit : pda::kWindowWideUnit;
-  plan->group_tokens = narrow ? n : std::min(n, plan->query_chunk * (pda::kWindowWideRows / pda::kMaxGroup));
+  plan->narrow = (int64_t)n * G <= pda::kWindowNarrowRows;
+  const int64_t quantum = plan->narrow ? pda::kWindowUnit : 2 * pda::kWindowUnit;  // (the wide kernel takes two blocks at a time)
+  plan->group_tokens = plan->narrow ? n : std::min(n, plan->query_chunk * (pda::kWindowWideRows / pda::kMaxGroup));
   plan->num_groups = (n + plan->group_tokens - 1) / plan->group_tokens;
   const int64_t len = longest_list(p, w, *plan);
   int64_t tokens = p->partition_tokens > 0 ? p->partition_tokens : partition_rule(p, *plan, len);
-  tokens = std::max<int64_t>(plan->unit, (std::min(tokens, len) + plan->unit - 1) / plan->unit * plan->unit);
+  tokens = std::max(quantum, (std::min(tokens, len) + quantum - 1) / quantum * quantum);
   const int64_t parts = std::max<int64_t>(1, (len + tokens - 1) / tokens);
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
   const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads;
@@ -149,12 +150,12 @@ int pda_decode_window(const pda_problem* prob, const pda_window* window, const v
   s.num_partitions = plan.info.num_partitions;
   s.slots_per_row = plan.info.num_partitions;
   s.num_regular_items = (int32_t)plan.items;
-  a.window = window->window;
-  a.sinks = window->num_sinks;
+  // (past every context they say the same, and the kernels' sums of positions stay inside int32)
+  a.window = std::min(window->window, prob->max_context_len + 1);
+  a.sinks = std::min(window->num_sinks, prob->max_context_len);
   a.group_tokens = plan.group_tokens;
   a.num_groups = plan.num_groups;
-  a.unit = plan.unit;
-  const hipError_t e = plan.unit == pda::kWindowUnit ? pda::launch_window(a, prob->head_dim, stream)
+  const hipError_t e = plan.narrow ? pda::launch_window(a, prob->head_dim, stream)
                                                      : pda::launch_window_wide(a, prob->head_dim, stream);
   if (e != hipSuccess) return PDA_ERR_HIP;
   if (plan.slots > 0 && pda::launch_window_merge(a, prob->head_dim, stream) != hipSuccess) return PDA_ERR_HIP;

@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kXcds = 8;
 constexpr int kStep = kStageBlocks * kBlockTokens;  // tokens
-static_assert(kStep == kWindowWideUnit && kWgChunks * 16 == kWindowWideRows, "the plan's units");
+static_assert(kStep == 2 * kWindowUnit && kWgChunks * 16 == kWindowWideRows, "the plan's units");
 
 template <int D>
 __global__ void __launch_bounds__(kWaves * kWaveSize) __attribute__((amdgpu_waves_per_eu(2)))
@@ -44,8 +44,8 @@ window_wide_kernel(const WindowArgs a) {
   int L = sa.lens[b];
   L = L < 0 ? 0 : (L > sa.max_context_len ? sa.max_context_len : L);
   const int i0 = gr * a.group_tokens, i1 = min(n, i0 + a.group_tokens);
-  const WindowSpan span = window_span(L, n, i0, i1, a.window, a.sinks, kStep);
-  const int per_part = sa.partition_tokens / kStep;
+  const WindowSpan span = window_span(L, n, i0, i1, a.window, a.sinks);
+  const int per_part = sa.partition_tokens / kBlockTokens;  // (even: whole steps)
   const int parts = (span.count() + per_part - 1) / per_part;
   auto out_row = [&](int i, int h) { return ((size_t)b * n + i) * Hq + (size_t)g * G + h; };
   if (p >= parts) {
@@ -71,8 +71,29 @@ window_wide_kernel(const WindowArgs a) {
   const int up_min = L - n + 1 + t0, up_max = L - n + t1;
   const int low_min = window_start(up_min, a.window), low_max = window_start(up_max, a.window);
   const int sinks = a.sinks;
-  auto whole = [&](int t) { return t + kStep <= up_min && (t + kStep <= sinks || t >= low_max); };
-  auto wanted = [&](int t) { return active && t < up_max && (t < sinks || t + kStep > low_min); };
+  // A step is two entries of the list, v and v + 1.  By where they stand: whole, every row of the tile sees
+  // every token of both (some that are so are not found: masking them changes nothing); wanted, some row sees
+  // some token.
+  const int at_sinks = span.sinks > 0 ? span.sinks : span.count();  // entries from block 0 on
+  auto entry = [&](int block) { return max(block, span.first) - span.first + span.sinks; };  // of the window's blocks
+  const int sinks_whole = min(min(sinks, max(up_min, 0)) / kBlockTokens, at_sinks);
+  const int whole_from = entry((low_max + kBlockTokens - 1) / kBlockTokens), whole_to = entry(max(up_min, 0) / kBlockTokens);
+  const int sinks_wanted = min((min(sinks, max(up_max, 0)) + kBlockTokens - 1) / kBlockTokens, at_sinks);
+  const int wanted_from = entry(low_min / kBlockTokens), wanted_to = entry((max(up_max, 0) + kBlockTokens - 1) / kBlockTokens);
+  auto whole = [&](int v) { return v + 1 < sinks_whole || (v >= whole_from && v + 1 < whole_to); };
+  auto wanted = [&](int v) { return active && (v < sinks_wanted || (v + 1 >= wanted_from && v < wanted_to)); };
+  // The first tokens of its blocks (past the list's end: past every row).
+  struct Step {
+    int a, b;
+  };
+  auto step_of = [&](int v) { return Step{span.token(v), v + 1 < span.count() ? span.token(v + 1) : span.end * kBlockTokens}; };
+  // The first x of 32 bits (all, or none).
+  auto first_bits = [](int x) { return x >= 32 ? 0xffffffffu : (1u << max(x, 0)) - 1u; };
+  // Bit c: whether a row with these limits sees token c + 4 hh of the step.
+  auto seen_bits = [&](Step k, int up_, int low_) {
+    auto from = [&](int base) { return first_bits(up_ - base) & (first_bits(sinks - base) | ~first_bits(low_ - base)); };
+    return (from(k.a + 4 * hh) & 0x0000ffffu) | (from(k.b - kBlockTokens + 4 * hh) & 0xffff0000u);
+  };
 
   float scale = sa.scale_log2;
   const unsigned flip = scale < 0.f ? 0x80008000u : 0u;
@@ -157,13 +178,10 @@ window_wide_kernel(const WindowArgs a) {
     top = max3(x, s[15], s[15]);
     asm volatile("" : "+v"(top));  // the MFMA results are first read in their own basic block
   };
-  // The first x of 32 bits (all, or none).
-  auto first_bits = [](int x) { return x >= 32 ? 0xffffffffu : (1u << max(x, 0)) - 1u; };
-  auto mask = [&](int tok0) {
-    if (!whole(tok0)) {  // wavefront-uniform: some row does not see some of these tokens
+  auto mask = [&](int v) {
+    if (!whole(v)) {  // wavefront-uniform: some row does not see some of these tokens
       asm volatile("");  // a branch: as selects the masking would run on every step
-      const int base = tok0 + 4 * hh;  // a bit for every token that the lane's row sees, then two instructions a score
-      const unsigned seen = first_bits(up - base) & (first_bits(sinks - base) | ~first_bits(low - base));
+      const unsigned seen = seen_bits(step_of(v), up, low);  // then two instructions a score
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const unsigned m = (unsigned)__builtin_amdgcn_sbfe((int)seen, 8 * (i / 4) + i % 4, 1);
@@ -176,9 +194,9 @@ window_wide_kernel(const WindowArgs a) {
   auto odd_halves = [](unsigned x) {
     return ((x & 0x7f80u) == 0x7f80u ? 0x0000ffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
   };
-  // Fold the step whose scores are in s (32 tokens from tok0 on, two blocks of
-  // a buffer), and form the scores of the next one (from next_tok0 on).
-  auto fold = [&](int tok0, const uint4* blocks, int next_tok0, const uint4* next_blocks) {
+  // Fold the step whose scores are in s (two blocks of a buffer), and form the scores of
+  // the next one.
+  auto fold = [&](int v, const uint4* blocks, const uint4* next_blocks) {
     auto v_frag = [&](int m, int t) {
       const uint16_t* v0 = reinterpret_cast<const uint16_t*>(blocks + S::kTilePieces + m * S::kBlockPieces) + tr_off[t];
       const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)v0));
@@ -195,7 +213,7 @@ window_wide_kernel(const WindowArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     // Where every element is finite, a token's probability of 0 leaves it out of a row that does not see it.
     bool odd = false;
-    if (!whole(tok0)) {  // wavefront-uniform
+    if (!whole(v)) {  // wavefront-uniform
       asm volatile("");
       typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
       u16x2_t top16 = {0, 0};
@@ -208,11 +226,12 @@ window_wide_kernel(const WindowArgs a) {
     }
     int any = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_ballot_w64(odd) != 0 ? 1 : 0);
     if (any) {
+      const Step at = step_of(v);
       // Infinities and NaN of tokens that only some rows see are left out of the product, and make the
       // rows that do see them NaN there, a token at a time (v - v is 0 for the others).
 #pragma unroll 1
       for (int x = 0; x < kStep; ++x) {
-        const int t = tok0 + x;
+        const int t = x < kBlockTokens ? at.a + x : at.b + x - kBlockTokens;
         if (!(t < up_max && (t < sinks || t >= low_min)) || (t < up_min && (t < sinks || t >= low_max))) continue;
         const bool mine = t < up && (t < sinks || t >= low);
         const int perm = D == 128 ? 4 * (x & 3) : 4 * ((x >> 1) & 1);
@@ -233,10 +252,8 @@ window_wide_kernel(const WindowArgs a) {
     asm volatile("" ::: "memory");  // (two branches of their own: as one they spilled 76 bytes a lane)
     any = __builtin_amdgcn_readfirstlane(any);
     if (any) {
-      // (V rows that no row of the tile sees are zeroed)
-      const int base = tok0 + 4 * hh;
-      auto bits = [&](int u, int l) { return first_bits(u - base) & (first_bits(sinks - base) | ~first_bits(l - base)); };
-      const unsigned some = bits(up_max, low_min), every = bits(up_min, low_max);
+      const Step at = step_of(v);  // (V rows that no row of the tile sees are zeroed)
+      const unsigned some = seen_bits(at, up_max, low_min), every = seen_bits(at, up_min, low_max);
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -299,21 +316,16 @@ window_wide_kernel(const WindowArgs a) {
       }
     s = ns;
     largest();
-    mask(next_tok0);
+    mask(v + kStageBlocks);
   };
 
-  // the tokens that the item's rows see: block j of a step is needed if it holds one of them
-  const int end = L - n + i1, lo = window_start(L - n + i0 + 1, a.window);
-  auto needed = [&](int j) { return j * kBlockTokens < end && (j * kBlockTokens < sinks || (j + 1) * kBlockTokens > lo); };
   const int v_end = min(span.count(), (p + 1) * per_part);
-  for (int vw = p * per_part; vw < v_end; vw += kWindow / kStageBlocks) {
-    const int nsteps = min(v_end - vw, kWindow / kStageBlocks);
+  for (int vw = p * per_part; vw < v_end; vw += kWindow) {
+    const int nsteps = (min(v_end - vw, kWindow) + kStageBlocks - 1) / kStageBlocks;
     // (as many as the steps and the loads issued past them read, by 64)
     const int n_ids = min(kWindow, (nsteps * kStageBlocks + kBuffers * kStageBlocks + kWaveSize) / kWaveSize * kWaveSize);
     for (int x = tid; x < n_ids; x += kWaves * kWaveSize) {
-      // past the end: the last step again (not folded); a step's block that nobody sees: the other one (masked)
-      const int j0 = span.token(vw + min(x / kStageBlocks, nsteps - 1), kStageBlocks) + x % kStageBlocks;
-      const int id = table_row[needed(j0) ? j0 : j0 ^ 1];
+      const int id = table_row[span.token(min(vw + x, v_end - 1)) / kBlockTokens];  // past the end: the last block again (masked, or not folded)
       const bool ok = (unsigned)id < (unsigned)sa.num_blocks;  // never read outside the pool
       bad |= !ok;
       st.ids[x] = ok ? id : 0;
@@ -328,8 +340,8 @@ window_wide_kernel(const WindowArgs a) {
       wait_loads<(kBuffers - 3) * kStepLoads>();
       __syncthreads();
       issue(step + kBuffers - 1);
-      const int tok0 = span.token(vw + step, kStep), next = span.token(vw + step + 1, kStep);
-      if (!wanted(tok0)) {  // wavefront-uniform
+      const int v = vw + kStageBlocks * step;
+      if (!wanted(v)) {  // wavefront-uniform
         ready = false;
         continue;
       }
@@ -338,12 +350,12 @@ window_wide_kernel(const WindowArgs a) {
         k_frags(st.buf[step % kBuffers][0], kf);
         s = scores(kf);
         largest();
-        mask(tok0);
+        mask(v);
       }
-      fold(tok0, st.buf[step % kBuffers][0], next, st.buf[(step + 1) % kBuffers][0]);
+      fold(v, st.buf[step % kBuffers][0], st.buf[(step + 1) % kBuffers][0]);
       ready = true;
     }
-    wait_loads<0>();
+  wait_loads<0>();
     __syncthreads();
   }
   const bool any_bad = __syncthreads_or(bad ? 1 : 0) != 0;  // (and the staging area is free)

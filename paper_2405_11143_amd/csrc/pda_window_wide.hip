@@ -355,39 +355,30 @@ window_wide_kernel(const WindowArgs a) {
       fold(v, st.buf[step % kBuffers][0], st.buf[(step + 1) % kBuffers][0]);
       ready = true;
     }
-  wait_loads<0>();
+    wait_loads<0>();
     __syncthreads();
   }
   const bool any_bad = __syncthreads_or(bad ? 1 : 0) != 0;  // (and the staging area is free)
 
   l_run += __shfl_xor(l_run, 32);
   const float mul = any_bad ? __builtin_nanf("") : parts == 1 && l_run > 0.f ? 1.f / l_run : 1.f;
-  const int swz = col & (D / 4 - 1);  // 16-byte units of a row permuted: conflict-free
-#pragma unroll
-  for (int t = 0; t < VT; ++t)
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      st.o[w][col][(8 * t + 2 * k + hh) ^ swz] =
-          f32x4_t{o[t][4 * k] * mul, o[t][4 * k + 1] * mul, o[t][4 * k + 2] * mul, o[t][4 * k + 3] * mul};
-  __syncthreads();
   if (!active) return;
-  for (int x = lane; x < kTileRows * (D / 4); x += kWaveSize) {
-    const int r32 = x / (D / 4);
-    const int d0 = 4 * (x % (D / 4));
-    const int c0 = r32 < 16 ? t0 : t0 + qc;  // the row's chunk
-    const int h = r32 & 15;
-    if (c0 >= t1 || h >= min(qc, t1 - c0) * G) continue;
-    const size_t row = out_row(c0 + h / G, h % G);
-    const f32x4_t v = st.o[w][r32][(d0 / 4) ^ (r32 & (D / 4 - 1))];
-    if (parts == 1)
-      store_nt4(sa.out + row * D + d0, v[0], v[1], v[2], v[3]);
-    else
-      *reinterpret_cast<f32x4_t*>(sa.part_o + (row * sa.slots_per_row + p) * D + d0) = v;
+  // Straight from the registers, 32 bytes of a row by two lanes at a time: L2 puts the
+  // lines together (through LDS in whole lines 1-7% longer, with the non-temporal hint 5-50%).
+  const bool real = (col & 15) < my_rows && (col < 16 || t0 + qc < t1);
+  const size_t my_row = out_row(my_i, my_r % G);
+  if (real) {
+    float* dst = (parts == 1 ? sa.out + my_row * D : sa.part_o + (my_row * sa.slots_per_row + p) * D) + 4 * hh;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<f32x4_t*>(dst + 32 * t + 8 * k) =
+            f32x4_t{o[t][4 * k] * mul, o[t][4 * k + 1] * mul, o[t][4 * k + 2] * mul, o[t][4 * k + 3] * mul};
   }
-  if (parts > 1 && hh == 0 && (col & 15) < my_rows && (col < 16 || t0 + qc < t1)) {
-    const size_t row = out_row(my_i, my_r % G);
-    sa.part_m[row * sa.slots_per_row + p] = m_run;
-    sa.part_l[row * sa.slots_per_row + p] = l_run;
+  if (parts > 1 && real && hh == 0) {
+    sa.part_m[my_row * sa.slots_per_row + p] = m_run;
+    sa.part_l[my_row * sa.slots_per_row + p] = l_run;
   }
 }
 

@@ -809,13 +809,17 @@ def _same_device(*tensors):
 
 def _zeros_like(t, stream):
     """Zeros of t's shape for a call on `stream`, filled on it too."""
+    return _cleared(_empty(t.shape, t.dtype, t.device, stream), stream)
+
+
+def _cleared(t, stream):
+    """t filled with zeros on `stream` (None: the current one)."""
     import torch
 
-    out = _empty(t.shape, t.dtype, t.device, stream)
     if stream is None:
-        return out.zero_()
+        return t.zero_()
     with torch.cuda.stream(_as_stream(stream, t.device)):
-        return out.zero_()
+        return t.zero_()
 
 
 def _check_fp8_cache(k_cache, v_cache, kv_scale):
@@ -1495,7 +1499,7 @@ def bind_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, posit
     if rc != PDA_OK:
         raise PdaError(rc, "pda_blocks_workspace_bytes")
     if workspace is None and ws.value > 0:
-        workspace = _zeros_like(_empty((ws.value,), torch.uint8, device, stream, result=False), stream)
+        workspace = _cleared(_empty((ws.value,), torch.uint8, device, stream, result=False), stream)
     workspace, ws_ptr, ws_bytes = _given_workspace(workspace, ws.value, device, stream)
     args = (ctypes.byref(pool), context_lens.data_ptr(), ctypes.byref(rows) if rows is not None else None, ws_ptr,
             ws_bytes, _stream_handle(stream, device))

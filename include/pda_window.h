@@ -34,9 +34,10 @@ typedef struct pda_window {
 
 /* Plan of pda_decode_window; prob->partition_tokens counts the tokens that are
  * read (a multiple of 16, rounded up to one of 32 for more than 32 query rows per KV head).
- * PDA_ERR_SHAPE also for what its launches cannot hold: 2^24 - 1 work items (partitions x
- * sequences x KV heads x groups of up to 128 query rows) or 2^26 - 4 output rows
- * where contexts are split. */
+ * PDA_ERR_SHAPE also for what its launches cannot hold: more than 2^24 - 1 work items
+ * (partitions x sequences x KV heads x groups of up to 128 query rows; with more than 32 rows per KV
+ * head, sequences x KV heads count as the next multiple of 8) or 2^26 - 4 output rows where
+ * contexts are split. */
 int pda_plan_window(const pda_problem *prob, const pda_window *window, pda_plan_info *plan);
 
 /* The attention of one step; out is fp32 [B][n][Hq][D], rows that see nothing are

@@ -81,7 +81,8 @@ int make_plan(const pda_problem* p, const pda_window* w, Plan* plan) {
   tokens = std::max(quantum, (std::min(tokens, len) + quantum - 1) / quantum * quantum);
   const int64_t parts = std::max<int64_t>(1, (len + tokens - 1) / tokens);
   // (each factor below 2^31, and rows of the whole batch too: two factors at a time)
-  const int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads;
+  int64_t pairs = (int64_t)p->num_seqs * p->num_kv_heads;
+  if (!plan->narrow) pairs = (pairs + pda::kWindowXcds - 1) / pda::kWindowXcds * pda::kWindowXcds;  // as launched
   if (pairs > kMostItems || pairs * plan->num_groups > kMostItems || parts * pairs * plan->num_groups > kMostItems)
     return PDA_ERR_SHAPE;
   if (parts > 1 && (int64_t)p->num_seqs * n * p->num_q_heads > kMostMergeRows) return PDA_ERR_SHAPE;

@@ -22,6 +22,7 @@ constexpr int kWindowTileRows = 16;     // query rows of an MFMA tile of the nar
 constexpr int kWindowNarrowRows = 32;   // most query rows of a work item there: two tiles
 constexpr int kWindowWideRows = 128;    // and of the wide kernel: 4 wavefronts of 32
 constexpr int kWindowUnit = kBlockTokens;
+constexpr int kWindowXcds = 8;          // the wide kernel launches a (sequence, KV head) for each, in turn
 
 // The blocks that new tokens [i0, i1) of a sequence of length L see something of, as a list: the
 // sinks' blocks [0, sinks), then [first, end).

@@ -14,7 +14,7 @@
 namespace pda {
 namespace {
 
-constexpr int kXcds = 8;
+constexpr int kXcds = kWindowXcds;
 constexpr int kStep = kStageBlocks * kBlockTokens;  // tokens
 static_assert(kStep == 2 * kWindowUnit && kWgChunks * 16 == kWindowWideRows, "the plan's units");
 

@@ -125,7 +125,9 @@ int main() {
         EXPECT((int64_t)seen.group_tokens * seen.num_groups >= n && (int64_t)seen.group_tokens * (seen.num_groups - 1) < n);
         EXPECT((int64_t)seen.group_tokens * s.group <= (wide_seen ? pda::kWindowWideRows : pda::kWindowNarrowRows));
         EXPECT(!wide_seen || s.partition_tokens % 32 == 0);
-        EXPECT(s.num_regular_items < (1 << 24));
+        EXPECT(s.num_regular_items < (1 << 24));  // (workgroups of 256 threads, less than 2^32)
+        const int64_t pairs = (int64_t)s.num_seqs * s.num_kv_heads;
+        EXPECT(!wide_seen || (pairs + 7) / 8 * 8 * seen.num_groups * s.num_partitions < (1 << 24));
         for (int k = 0; k < 8; ++k) {
           const int L = k == 0 ? p.max_context_len : (int)(next_u32() % ((uint32_t)p.max_context_len + 1));
           const int gr = k < 2 ? seen.num_groups - 1 : (int)(next_u32() % seen.num_groups);

@@ -180,6 +180,8 @@ def call_window(p=None, w=(64, 4), q=SOME, k=SOME, v=SOME, bt=SOME, lens=SOME, s
     (dict(p=prob(partition_tokens=16), ws=None, size=0), P.PDA_ERR_WORKSPACE), (dict(p=prob(partition_tokens=16), size=64), P.PDA_ERR_WORKSPACE),
     (dict(p=prob(partition_tokens=16), ws=SOME + 4), P.PDA_ERR_ALIGNMENT),
     (dict(p=prob(num_seqs=1 << 23, num_q_heads=2, num_kv_heads=2)), P.PDA_ERR_SHAPE),
+    # groups of 8 tokens, launched for 8 (sequence, KV head)s: a workgroup too many
+    (dict(p=prob(num_seqs=1, num_q_heads=16, num_kv_heads=1, num_query_tokens=1 << 24)), P.PDA_ERR_SHAPE),
     (dict(p=prob(num_seqs=0), q=None, k=None, v=None, bt=None, lens=None, out=None, ws=None, size=0), P.PDA_OK)])
 def test_window_refuses(kw, status):
     assert call_window(**{**dict(p=prob()), **kw}) == status

@@ -20,7 +20,8 @@
  * contiguous: the parts of a fused projection's rows can be used where they lie.
  * num_kv_heads 0: no keys.  dtype PDA_DTYPE_BF16 or PDA_DTYPE_F32, the same for all rows of a
  * call.  D is a multiple of 8, at most 512; pointers and rows are 16-byte aligned.
- * Elements are below 2^59 in magnitude (their squares are summed in fp32).
+ * Elements are below 2^59 in magnitude (their squares are summed in fp32); with eps 0 a
+ * row's largest is above 2^-59.
  * `positions` is device int32 [T], or [num_axes] rows of T.  A token whose position
  * (on the first axis) is negative is padding: its rows are neither read nor
  * written.  Positions on further axes may have either sign.

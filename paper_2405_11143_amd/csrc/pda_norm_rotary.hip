@@ -7,6 +7,12 @@
 // per lane; a row's U lanes are neighbours, so its sum of squares is a few DPP steps.  The rows
 // of two steps are in flight, the first two loaded before the angles are formed.
 // Nothing waits for another wavefront.
+//
+// Measured, bf16 (a copy of 1 GiB runs at 5.1 TB/s here): 16384 tokens of 32 + 8 heads of 128, with
+// norms, 59 us, 5.6 TB/s; their gradient 103 us, 4.8 TB/s; 26000 tokens of 28 + 4 heads with their
+// values into the cache 96 us, 5.0 TB/s; 6000 tokens of 28 + 4 heads, three axes, rotation alone, 22.3 us
+// (17.8 with rows that the last-level cache holds); 4097 of 16 + 16 heads of 64 in fp32, two axes,
+// turned back, 18.8 us (16.1); 256 tokens of a decode step into the cache 5.1 us, of which the launch is 4.4.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,8 +26,7 @@ constexpr int kWavesHere = kThreads / kWaveSize;
 constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
 constexpr int kMaxDim = 512;
 constexpr int kXcds = 8;
-constexpr int kFewWaves = 4096;    // wavefronts that fewer tokens are split into
-constexpr int kTwoTokens = 16384;  // tokens below this, and above the other, are split in two
+constexpr int kFewWaves = 4096;  // wavefronts that fewer tokens are split into
 
 // 8 elements as they lie in memory.
 template <typename T>
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryA
     int64_t t = x;
     int part = 0;
     if (parts > 1) {
-      t = (uint32_t)x / (uint32_t)parts;  // (few tokens)
+      t = (uint64_t)x >> 32 ? x / parts : (uint32_t)x / (uint32_t)parts;
       part = (int)(x - t * parts);
     } else if (STORE) {
       // 16 neighbouring tokens, which fill whole lines of a block's keys together, on one XCD: 4
@@ -225,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryA
                  row_at + (d1 + v * (v1 - d1)) * (unsigned)sizeof(T));
     };
     // A step's rows; `next` is loaded into its place.  Loads go out before the stores: waiting for a load waits
-    // for every store before it, too.
+    // for every store before it, too (16384 tokens of 32 + 8 heads 80 us with the loads behind, 63 so).
     auto finish = [&](int i, RawShare<T, FULL>& raw, int next) __attribute__((always_inline)) {
       if (i >= steps) return;
       const RowStep s = row_step(i, q_steps, k_steps);
@@ -285,7 +290,9 @@ __global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryA
 }
 
 // The gradient.  Every lane sums its elements' h u over its rows and tokens; at the end
-// the wavefront's rows are summed by shuffles, the wavefronts through LDS.
+// the wavefront's rows are summed by shuffles, the wavefronts through LDS.  One step's rows are in flight
+// and three wavefronts share a SIMD: 103 us for 16384 tokens of 32 + 8 heads of 128; with two steps in
+// flight 116, with four wavefronts 139.
 template <typename T, int U, bool FULL>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) norm_rotary_grad_kernel(const NormRotaryArgs a) {
   constexpr int RPW = kWaveSize / U;
@@ -430,13 +437,18 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const float* part
 }
 
 // Wavefronts that share a token: one where tokens are many, up to one for each of its steps where
-// they are few; as many as make the last trip a full one, nearly.
-int parts_of(int U, int64_t tokens, int q_heads, int key_heads, int value_heads) {
+// they are few; as many as make the last trip a full one, nearly.  Two for many tokens too where
+// they are normed, rows are of up to 8 lanes and a token has 5 steps or more.  us, one / two, bf16: 16384
+// tokens of 32 + 8 heads of 128 (5 steps) 61.0 / 58.9, 50000 180 / 165, 8000 33.8 / 32.9; in fp32 128.1 /
+// 124.5; 20000 of 40 + 8 88.1 / 82.3; 6000 of 64 + 8 44.6 / 41.9; but 30000 of 12 + 2 (3 steps) 48.6 /
+// 61.9, 12000 of 16 + 4 of 256 48.9 / 51.2, rotation alone of 14000 of 28 + 4 43.1 / 45.7, 26000 of
+// 28 + 4 into the cache, whose neighbours then do not fill lines together, 96 / 112.
+int parts_of(int U, bool halved, int64_t tokens, int q_heads, int key_heads, int value_heads) {
   const int rpw = kWaveSize / U;
   auto steps_of = [&](int heads) { return (heads + rpw - 1) / rpw; };
   const int steps = steps_of(q_heads) + steps_of(key_heads) + steps_of(value_heads);
-  const int64_t ways = tokens > kFewWaves && tokens < kTwoTokens ? 2 : std::max<int64_t>(1, kFewWaves / tokens);
-  const int most = (int)std::min<int64_t>(steps, ways);
+  const int64_t many = halved && U <= 8 && steps >= 5 && tokens > kFewWaves ? 2 : 1;
+  const int most = (int)std::min<int64_t>(steps, std::max(many, kFewWaves / tokens));
   const int trips = (steps + most - 1) / most;
   return (steps + trips - 1) / trips;
 }
@@ -467,7 +479,7 @@ void launch_apply(const NormRotaryArgs& a, hipStream_t stream) {
   with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
     constexpr bool FULL = decltype(full)::value;
-    const int parts = parts_of(U, a.num_tokens, a.q.heads, a.k.heads, 0);
+    const int parts = parts_of(U, NORM, a.num_tokens, a.q.heads, a.k.heads, 0);
     const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
     if constexpr (sizeof(T) == 2 && FULL && U >= 8) {
       if (a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim)) {
@@ -494,7 +506,7 @@ hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream
   with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
     if constexpr (U <= 8 && decltype(full)::value) {  // head_dim 64 and 128
-      const int parts = parts_of(U, a.num_tokens, a.q.heads, a.k.heads, a.k.heads);
+      const int parts = parts_of(U, false, a.num_tokens, a.q.heads, a.k.heads, a.k.heads);
       const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
       auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, parts); };
       auto launch_kind = [&](auto normed) {

@@ -9,11 +9,11 @@
 // its rows sees.  The items of one (sequence, KV head) run on one XCD next to each
 // other: neighbouring groups see almost the same tokens, which then come from its L2.
 //
-// Bound by the matrix units: with P in two bf16 parts a step is 3 products where the mathematics
-// has 2.  512 new tokens of 32 sequences (32 / 8 heads of 128) over a window of 1024: 495 us, 555
-// TFLOP/s by what the rows see, 860 by what is issued with the masked corners; 545 with
-// steps of 32 aligned tokens and probabilities cut off, 505 with rows stored through LDS.  Rounding P to nearest
-// costs 1.5% and halves the error.
+// Bound by the matrix units: with P in three bf16 parts a step is 4 products where the
+// mathematics has 2.  512 new tokens of 32 sequences (32 / 8 heads of 128) over a window of 1024: 551 us, 500
+// TFLOP/s by what the rows see, 1030 by what is issued.  With P in two parts, rounded to nearest, 485 us and
+// results 2.4e-6 of their norm off instead of 4.5e-7 (plain fp32 operations: 7e-7); three parts rounded to
+// nearest 570.  Before, with two parts: steps of 32 aligned tokens 10% more, rows stored through LDS 2%.
 #include "pda_wide.h"
 #include "pda_window_internal.h"
 
@@ -292,34 +292,34 @@ window_wide_kernel(const WindowArgs a) {
       for (int t = 0; t < VT; ++t) o[t] *= al;
     }
     const f32x16_t ns = scores(kf);
-    bf16x8_t bh[2], bl[2];
+    // The probabilities in three bf16 parts, all 24 bits: cut off, so that what is left is exact.
+    bf16x8_t part[2][3];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       float pr[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) pr[i] = exp2_fast(fmaf(s[8 * m + i], scale, -ref));
       l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-      unsigned hw[4], lw[4];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {  // rounded to nearest, and what is left of it: half the error of cutting off
-        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-        const bf16x2_t h2 = {(__bf16)pr[2 * h], (__bf16)pr[2 * h + 1]};
-        hw[h] = __builtin_bit_cast(unsigned, h2);
-        const bf16x2_t l2 = {(__bf16)(pr[2 * h] - __uint_as_float(hw[h] << 16)),
-                             (__bf16)(pr[2 * h + 1] - __uint_as_float(hw[h] & 0xffff0000u))};
-        lw[h] = __builtin_bit_cast(unsigned, l2);
+      for (int x = 0; x < 3; ++x) {
+        unsigned w[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          w[h] = pack_halves(__float_as_uint(pr[2 * h]), __float_as_uint(pr[2 * h + 1]), true);
+          if (x == 2) continue;
+          pr[2 * h] -= __uint_as_float(__float_as_uint(pr[2 * h]) & 0xffff0000u);
+          pr[2 * h + 1] -= __uint_as_float(__float_as_uint(pr[2 * h + 1]) & 0xffff0000u);
+        }
+        part[m][x] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
       }
-      bh[m] = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
-      bl[m] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int t = 0; t < VT; ++t) {
-        const bf16x8_t av = __builtin_bit_cast(bf16x8_t, vf[m][t]);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bh[m], o[t], 0, 0, 0);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bl[m], o[t], 0, 0, 0);
-      }
+      for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[m][t]), part[m][x], o[t], 0, 0, 0);
     s = ns;
     largest();
     mask(v + kStageBlocks);

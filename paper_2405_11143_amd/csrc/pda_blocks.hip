@@ -170,19 +170,19 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const BlocksArgs a) 
 }
 
 // The whole resize, every workgroup with all the sums: the first workgroup moves up to kOwn of each
-// row's ids, a row to a thread; what is left is shared out a row to a wavefront, and the slot map
+// row's ids, a row to a thread; what is left is shared out, a row to a wavefront or several, and the slot map
 // a token row to a thread.  An id is read from where it was before the call, so no workgroup reads
 // what another has written.  Two calls, us, against the two kernels: 256 sequences of up to 4096
-// tokens, 5 new ones each and back, 11.9 / 16.1 (of which 4.4 a call are the calls themselves);
-// all of their 33000 blocks granted and put back 17.4 / 16.1.  With one workgroup for everything the
-// first took 9.8 and the second 32.
+// tokens, 5 new ones each and back, 11.8 / 16.1 (of which 4.4 a call are the calls themselves);
+// all of their 33000 blocks granted and put back 16.3 / 16.1.  With one workgroup for everything the
+// first took 9.8 and the second 32.  Two rows of 3750 blocks 19, with a wavefront to a row 29.
 constexpr int kOneSeqs = kPlanThreads;
 constexpr int kOwn = 4;
-constexpr int64_t kEntriesEach = 8192, kRowsEach = 2048;  // of a workgroup
+constexpr int64_t kEntriesEach = 4096, kRowsEach = 1024;  // of a workgroup
 // With more token rows than this the two kernels take over, whose threads need not find
 // their row's sequence.  Admitted and released in two calls, us, one launch each / two: 32000
-// rows of 8 sequences 14.5 / 19.0, 25600 of 256 16.4 / 16.6, 64000 of 64 16.1 / 16.7, 115200
-// of 128 18.7 / 16.9, 128000 of 256 16.6 / 16.4.
+// rows of 8 sequences 14.9 / 19.0, 25600 of 256 14.9 / 16.6, 64000 of 64 15.8 / 16.7, 115200
+// of 128 17.4 / 17.2, 1 million of 512 24.5 / 20.4.
 constexpr int kOneRows = 65536;
 constexpr int64_t kMostGroups = 128;
 constexpr int kAhead = 4;  // entries of a row that a lane has in flight
@@ -291,10 +291,13 @@ __global__ void __launch_bounds__(kPlanThreads) resize_kernel(const BlocksArgs a
   if (all_rests > 0) {  // (the same for all threads)
     if (more) rest[place] = Rest{b, my.from, grows ? my.count : -my.count, my.rank};
     __syncthreads();
-    for (int i = group * kPlanWaves + wave; i < all_rests; i += groups * kPlanWaves) {
-      const Rest x = rest[i];
+    const int waves = groups * kPlanWaves;
+    const int share = max(__builtin_clz(all_rests) - __builtin_clz(waves) - 1, 0);  // 2^share wavefronts to a row
+    for (int i = group * kPlanWaves + wave; i < all_rests << share; i += waves) {
+      const Rest x = rest[i >> share];
       const Moves m{x.row, x.from, abs(x.count), x.rank, x.count > 0};
-      for (int e0 = kOwn + lane; e0 < m.count; e0 += kAhead * kWaveSize) {
+      const int part = i & ((1 << share) - 1);
+      for (int e0 = kOwn + part * kAhead * kWaveSize + lane; e0 < m.count; e0 += kAhead * kWaveSize << share) {
         int id[kAhead];
 #pragma unroll
         for (int h = 0; h < kAhead; ++h)

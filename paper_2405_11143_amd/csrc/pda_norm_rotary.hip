@@ -27,6 +27,11 @@ constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 th
 constexpr int kMaxDim = 512;
 constexpr int kXcds = 8;
 constexpr int kFewWaves = 4096;  // wavefronts that fewer tokens are split into
+// From so many tokens on, rows of whole cache lines go out with the non-temporal hint.  32 + 8 heads of 128,
+// us, without / with: 256 tokens 5.0 / 5.0, 512 5.4 / 4.9, 1024 7.2 / 6.2, 1500 9.1 / 7.6, 2500 13.8 / 10.6, 16384 65.2
+// / 59.2; into the cache 26000 of 28 + 4 101.7 / 96.0.  With a kernel behind it that reads the queries the
+// two take 9.2 / 8.9 for 512, 12.9 / 11.7 for 1024, 20.2 / 21.7 for 3000.
+constexpr int kHintTokens = 512;
 
 // 8 elements as they lie in memory.
 template <typename T>
@@ -482,7 +487,7 @@ void launch_apply(const NormRotaryArgs& a, hipStream_t stream) {
     const int parts = parts_of(U, NORM, a.num_tokens, a.q.heads, a.k.heads, 0);
     const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
     if constexpr (sizeof(T) == 2 && FULL && U >= 8) {
-      if (a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim)) {
+      if (a.num_tokens >= kHintTokens && whole_lines(a.rot, a.head_dim)) {
         hipLaunchKernelGGL((norm_rotary_kernel<T, U, FULL, NORM, false, true>), grid, threads, 0, stream, a, parts);
         return;
       }
@@ -502,7 +507,7 @@ hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, hipStream_t st
 }
 
 hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream) {
-  const bool nt = a.num_tokens >= kManyTokens && whole_lines(a.rot, a.head_dim);
+  const bool nt = a.num_tokens >= kHintTokens && whole_lines(a.rot, a.head_dim);
   with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
     if constexpr (U <= 8 && decltype(full)::value) {  // head_dim 64 and 128

@@ -9,7 +9,7 @@
 // Nothing waits for another wavefront.
 //
 // Measured, bf16 (a copy of 1 GiB runs at 5.1 TB/s here): 16384 tokens of 32 + 8 heads of 128, with
-// norms, 59 us, 5.6 TB/s; their gradient 103 us, 4.8 TB/s; 26000 tokens of 28 + 4 heads with their
+// norms, 59 us, 5.6 TB/s; their gradient 100 us, 4.9 TB/s; 26000 tokens of 28 + 4 heads with their
 // values into the cache 96 us, 5.0 TB/s; 6000 tokens of 28 + 4 heads, three axes, rotation alone, 22.3 us
 // (17.8 with rows that the last-level cache holds); 4097 of 16 + 16 heads of 64 in fp32, two axes,
 // turned back, 18.8 us (16.1); 256 tokens of a decode step into the cache 5.1 us, of which the launch is 4.4.
@@ -296,10 +296,11 @@ __global__ void __launch_bounds__(kThreads) norm_rotary_kernel(const NormRotaryA
 
 // The gradient.  Every lane sums its elements' h u over its rows and tokens; at the end
 // the wavefront's rows are summed by shuffles, the wavefronts through LDS.  One step's rows are in flight
-// and three wavefronts share a SIMD: 103 us for 16384 tokens of 32 + 8 heads of 128; with two steps in
-// flight 116, with four wavefronts 139.
-template <typename T, int U, bool FULL>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) norm_rotary_grad_kernel(const NormRotaryArgs a) {
+// and three wavefronts share a SIMD: 104 us for 16384 tokens of 32 + 8 heads of 128; with two steps in
+// flight 116, with four wavefronts 139.  NT: the rows go out with the non-temporal hint: 100, 1500 tokens 19.9 -> 18.1.
+template <typename T, int U, bool FULL, bool NT>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3)))
+norm_rotary_grad_kernel(const NormRotaryArgs a, int parts) {
   constexpr int RPW = kWaveSize / U;
   __shared__ union {
     float2 turns[kWavesHere][kMaxDim / 2];
@@ -325,7 +326,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
   const int d0 = w.d0, d1 = w.d1;
   const bool has0 = d0 < D, has1 = d1 < D;
   const unsigned row_at = row * D * (unsigned)sizeof(T);
-  for (int64_t t = (int64_t)blockIdx.x * kWavesHere + wave; t < a.num_tokens; t += (int64_t)gridDim.x * kWavesHere) {
+  for (int64_t x = (int64_t)blockIdx.x * kWavesHere + wave; x < a.num_tokens * (int64_t)parts;
+       x += (int64_t)gridDim.x * kWavesHere) {
+    int64_t t = x;
+    int part = 0;
+    if (parts > 1) {
+      t = (uint32_t)x / (uint32_t)parts;  // (few tokens)
+      part = (int)(x - t * parts);
+    }
     const int pos = a.positions[t];
     if (pos < 0) continue;  // padding
     const uint64_t q_at = (uint64_t)(static_cast<const T*>(a.q.in) + t * a.q.in_stride);
@@ -386,14 +394,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
       }
       char* out = reinterpret_cast<char*>(is_q ? static_cast<T*>(a.q.out) + t * a.q.out_stride : static_cast<T*>(a.k.out) + t * a.k.out_stride) +
                   (is_q ? i : i - q_steps) * (RPW * D * (int)sizeof(T));
-      if (FULL || has0) store8<false>(reinterpret_cast<T*>(out + (row_at + d0 * (unsigned)sizeof(T))), p);
-      if (FULL || has1) store8<false>(reinterpret_cast<T*>(out + (row_at + d1 * (unsigned)sizeof(T))), q);
+      if (FULL || has0) store8<NT>(reinterpret_cast<T*>(out + (row_at + d0 * (unsigned)sizeof(T))), p);
+      if (FULL || has1) store8<NT>(reinterpret_cast<T*>(out + (row_at + d1 * (unsigned)sizeof(T))), q);
     };
     RawShare<T, FULL> xs, gs;
-    load(0, xs, gs);
+    load(part, xs, gs);
     form_turns(a, R, t, pos, turns);
     w.read(turns);
-    for (int i = 0; i < steps; ++i) finish(i, xs, gs, i + 1);
+    for (int i = part; i < steps; i += parts) finish(i, xs, gs, i + parts);
     wave_sync();  // the next token's turns take the same place
   }
   __syncthreads();  // (the sums take the turns' place)
@@ -449,13 +457,9 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const float* part
 // 61.9, 12000 of 16 + 4 of 256 48.9 / 51.2, rotation alone of 14000 of 28 + 4 43.1 / 45.7, 26000 of
 // 28 + 4 into the cache, whose neighbours then do not fill lines together, 96 / 112.
 int parts_of(int U, bool halved, int64_t tokens, int q_heads, int key_heads, int value_heads) {
-  const int rpw = kWaveSize / U;
-  auto steps_of = [&](int heads) { return (heads + rpw - 1) / rpw; };
-  const int steps = steps_of(q_heads) + steps_of(key_heads) + steps_of(value_heads);
-  const int64_t many = halved && U <= 8 && steps >= 5 && tokens > kFewWaves ? 2 : 1;
-  const int most = (int)std::min<int64_t>(steps, std::max(many, kFewWaves / tokens));
-  const int trips = (steps + most - 1) / most;
-  return (steps + trips - 1) / trips;
+  const int steps = row_steps(q_heads, U) + row_steps(key_heads, U) + row_steps(value_heads, U);
+  const bool two = halved && U <= 8 && steps >= 5 && tokens > kFewWaves;
+  return wave_parts(steps, two ? 2 : kFewWaves / tokens);
 }
 
 unsigned grid_of(int64_t tokens, int parts) {
@@ -468,12 +472,12 @@ void with_lanes(int head_dim, F&& f) {
   auto with = [&](auto lanes) {
     head_dim == 16 * decltype(lanes)::value ? f(lanes, std::true_type()) : f(lanes, std::false_type());
   };
-  const int shares = row_shares(head_dim);
-  if (shares <= 4)
+  const int lanes = row_lanes(head_dim);
+  if (lanes == 4)
     with(std::integral_constant<int, 4>());
-  else if (shares <= 8)
+  else if (lanes == 8)
     with(std::integral_constant<int, 8>());
-  else if (shares <= 16)
+  else if (lanes == 16)
     with(std::integral_constant<int, 16>());
   else
     with(std::integral_constant<int, 32>());
@@ -528,16 +532,17 @@ hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream
 }
 
 hipError_t launch_norm_rotary_backward(const NormRotaryArgs& a, int dtype, hipStream_t stream) {
-  const int groups = grad_groups(a.num_tokens);
+  const int parts = grad_parts(a.num_tokens, a.q.heads, a.head_dim), groups = grad_groups(a.num_tokens, parts);
   if (groups > 0)
     with_lanes(a.head_dim, [&](auto lanes, auto full) {
       constexpr int U = decltype(lanes)::value;
       constexpr bool FULL = decltype(full)::value;
-      const dim3 threads(kThreads);
-      if (dtype == PDA_DTYPE_BF16)
-        hipLaunchKernelGGL((norm_rotary_grad_kernel<__bf16, U, FULL>), dim3(groups), threads, 0, stream, a);
-      else
-        hipLaunchKernelGGL((norm_rotary_grad_kernel<float, U, FULL>), dim3(groups), threads, 0, stream, a);
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(kThreads), 0, stream, a, parts); };
+      if (dtype != PDA_DTYPE_BF16) return launch(norm_rotary_grad_kernel<float, U, FULL, false>);
+      if constexpr (FULL && U >= 8) {
+        if (a.num_tokens >= kHintTokens && whole_lines(a.rot, a.head_dim)) return launch(norm_rotary_grad_kernel<__bf16, U, FULL, true>);
+      }
+      launch(norm_rotary_grad_kernel<__bf16, U, FULL, false>);
     });
   if (a.d_weight[0] || a.d_weight[1])
     hipLaunchKernelGGL(weight_grad_kernel, dim3(2 * a.head_dim / kSumColumns), dim3(kThreads), 0, stream, a.part, groups,

@@ -121,7 +121,8 @@ int pda_norm_rotary_workspace_bytes(int32_t num_tokens, int32_t num_q_heads, int
   if (num_tokens < 0 || head_dim < 1 || num_q_heads < 1) return PDA_ERR_SHAPE;
   if (head_dim % 8 != 0 || head_dim > kMaxHeadDim) return PDA_ERR_UNSUPPORTED;
   PDA_CHECK(check_sizes(num_q_heads, num_kv_heads, head_dim, PDA_DTYPE_F32));
-  *bytes = (size_t)pda::grad_groups(num_tokens) * 2 * head_dim * sizeof(float);
+  const int parts = pda::grad_parts(num_tokens, num_q_heads, head_dim);
+  *bytes = (size_t)pda::grad_groups(num_tokens, parts) * 2 * head_dim * sizeof(float);
   return PDA_OK;
 }
 

@@ -19,9 +19,9 @@ constexpr int64_t kMostMergeRows = 4 * kMostItems;   // the merge: workgroups of
 // 128, us, this rule / whole / the best of partitions of 128 to 2064: 1 sequence with a window of 512 7.9
 // / 7.9 / 9.3, of 1024 10.3 / 12.9 / 10.4, of 4096 13.1 / - / 12.7; 4: 8.9 / 8.9 / 10.1, 11.2 /
 // 13.5 / 11.1, 17.9 / - / 18.0; 8: 9.2 / 9.2 / 10.7, 12.8 / 14.1 / 13.0, 26.9 / - / 27.0; 16 of 1024
-// 15.7 / 15.7 / 17.7, of 4096 45.8 / - / 46.0.  64 new tokens over a window of 1024: 1 sequence whole
-// 44.8, in 288s 24.6, in 128s 21.9; 4 45.7, 30.3, 41.7; 8 47.2, 43.1, 66.8; 512 new ones of 2
-// (256 items) 51.0 whole, 68.5 in 512s.
+// 15.7 / 15.7 / 17.7, of 4096 45.8 / - / 46.0; 24 of 1024 18.5 / 18.5 / 22.2.  64 new tokens over a window
+// of 1024, this rule / whole / in 288s / in 128s: 1 sequence 18.6 / 46.2 / 22.0 / 18.7; 2 21.7 / 46.6 / 23.9 / 25.3;
+// 4 28.9 / 46.7 / 27.9 / 40.4; 8 43.4 / 48.1 / 42.9 / 63.6; 512 new ones of 2 (256 items) 51 whole, 69 in 512s.
 constexpr int64_t kNarrowAtOnce = 256, kNarrowLeast = 176, kNarrowGain = 600;
 constexpr int64_t kWideAtOnce = 512, kWideLeast = 256, kWideFew = 128, kWideGain = 400;
 

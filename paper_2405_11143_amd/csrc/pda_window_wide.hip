@@ -12,7 +12,8 @@
 // Bound by the matrix pipes (49% busy, at 1.9 GHz) and vector issue (50%) beside each other: with P in three
 // bf16 parts a step is 4 products where the mathematics has 2.  512 new tokens of 32 sequences (32 / 8
 // heads of 128) over a window of 1024: 551 us, 500 TFLOP/s by what the rows see, 1030 by what is
-// issued, 85% of what a large library product reaches.  With P in two parts, rounded to nearest, 485 us and
+// issued, 85% of what a large library product reaches; over whole contexts of 4096, where few steps are masked
+// and a workgroup takes 128, 570 and 1140, 94%.  A barrier for every second step only: 1% less time.  With P in two parts, rounded to nearest, 485 us and
 // results 2.4e-6 of their norm off instead of 4.5e-7 (plain fp32 operations: 7e-7); three parts rounded to
 // nearest 570.  Before, with two parts: steps of 32 aligned tokens 10% more, rows stored through LDS 2%.
 #include "pda_wide.h"

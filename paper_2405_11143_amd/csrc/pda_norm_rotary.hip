@@ -26,6 +26,7 @@ constexpr int kWavesHere = kThreads / kWaveSize;
 constexpr int kMaxGrid = 1 << 20;  // workgroups (a launch has less than 2^32 threads); they loop over the rest
 constexpr int kMaxDim = 512;
 constexpr int kXcds = 8;
+constexpr int kComputeUnits = 256;
 constexpr int kFewWaves = 4096;  // wavefronts that fewer tokens are split into
 // From so many tokens on, rows of whole cache lines go out with the non-temporal hint.  32 + 8 heads of 128,
 // us, without / with: 256 tokens 5.0 / 5.0, 512 5.4 / 4.9, 1024 7.2 / 6.2, 1500 9.1 / 7.6, 2500 13.8 / 10.6, 16384 65.2
@@ -456,14 +457,20 @@ __global__ void __launch_bounds__(kThreads) weight_grad_kernel(const float* part
 // 124.5; 20000 of 40 + 8 88.1 / 82.3; 6000 of 64 + 8 44.6 / 41.9; but 30000 of 12 + 2 (3 steps) 48.6 /
 // 61.9, 12000 of 16 + 4 of 256 48.9 / 51.2, rotation alone of 14000 of 28 + 4 43.1 / 45.7, 26000 of
 // 28 + 4 into the cache, whose neighbours then do not fill lines together, 96 / 112.
-int parts_of(int U, bool halved, int64_t tokens, int q_heads, int key_heads, int value_heads) {
-  const int steps = row_steps(q_heads, U) + row_steps(key_heads, U) + row_steps(value_heads, U);
+int parts_of(int U, bool halved, int64_t tokens, int steps) {
   const bool two = halved && U <= 8 && steps >= 5 && tokens > kFewWaves;
   return wave_parts(steps, two ? 2 : kFewWaves / tokens);
 }
 
-unsigned grid_of(int64_t tokens, int parts) {
-  return (unsigned)std::min<int64_t>(kMaxGrid, (tokens * parts + kWavesHere - 1) / kWavesHere);
+// Workgroups: one for every 4 wavefronts' turns; where rows fill less than three quarters of their steps, so that
+// instructions bound the kernel, only as many as run at once (4 or 5 wavefronts on a SIMD), which loop over the rest.
+// us, so / in rounds: 30000 tokens of 12 + 2 heads of 128 43.4 / 49.0, 60000 of 8 + 2 of 64 52.7 / 64.4, 20000 of 16 + 1
+// of 128 36.8 / 38.1; into the cache 22000 of 12 + 2 45.6 / 51.2, 54000 of 8 + 2 of 64 80 / 91; but 16384 of 32 + 8
+// of 128, all full, 62.4 / 59.1, 20000 of 24 + 8 60.3 / 58.3, into the cache 22000 of 16 + 16 of 64 68.2 / 62.8.
+unsigned grid_of(int64_t tokens, int parts, int U, int rows, int steps, int waves_at_once) {
+  const bool sparse = rows * U * 4 < kWaveSize * steps * 3;
+  const int64_t most = sparse ? kComputeUnits * 4 * waves_at_once / kWavesHere : kMaxGrid;
+  return (unsigned)std::min<int64_t>(most, (tokens * parts + kWavesHere - 1) / kWavesHere);
 }
 
 // f(U, FULL) as integral constants: the lanes that a row of head_dim elements takes.
@@ -488,8 +495,8 @@ void launch_apply(const NormRotaryArgs& a, hipStream_t stream) {
   with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
     constexpr bool FULL = decltype(full)::value;
-    const int parts = parts_of(U, NORM, a.num_tokens, a.q.heads, a.k.heads, 0);
-    const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
+    const int steps = row_steps(a.q.heads, U) + row_steps(a.k.heads, U), parts = parts_of(U, NORM, a.num_tokens, steps);
+    const dim3 grid(grid_of(a.num_tokens, parts, U, a.q.heads + a.k.heads, steps, sizeof(T) == 2 ? 5 : 4)), threads(kThreads);
     if constexpr (sizeof(T) == 2 && FULL && U >= 8) {
       if (a.num_tokens >= kHintTokens && whole_lines(a.rot, a.head_dim)) {
         hipLaunchKernelGGL((norm_rotary_kernel<T, U, FULL, NORM, false, true>), grid, threads, 0, stream, a, parts);
@@ -515,8 +522,8 @@ hipError_t launch_norm_rotary_append(const NormRotaryArgs& a, hipStream_t stream
   with_lanes(a.head_dim, [&](auto lanes, auto full) {
     constexpr int U = decltype(lanes)::value;
     if constexpr (U <= 8 && decltype(full)::value) {  // head_dim 64 and 128
-      const int parts = parts_of(U, false, a.num_tokens, a.q.heads, a.k.heads, a.k.heads);
-      const dim3 grid(grid_of(a.num_tokens, parts)), threads(kThreads);
+      const int steps = row_steps(a.q.heads, U) + 2 * row_steps(a.k.heads, U), parts = parts_of(U, false, a.num_tokens, steps);
+      const dim3 grid(grid_of(a.num_tokens, parts, U, a.q.heads + 2 * a.k.heads, steps, 4)), threads(kThreads);
       auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, parts); };
       auto launch_kind = [&](auto normed) {
         constexpr bool NORM = decltype(normed)::value;

@@ -41,6 +41,18 @@ def test_append_of_many_tokens(T, Hq, Hkv, D, R):
     heads.test_append(T, Hq, Hkv, D, R, dict(axes=2, offset=1.0))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,R", [(4, 1, 128, 128), (8, 2, 64, 32), (32, 8, 128, 128)])
+def test_many_tokens_in_place(Hq, Hkv, D, R):
+    """Wavefronts that loop over tokens, and ones that do not: over the rows themselves the same bits as beside them."""
+    c = heads.Case(12001, Hq, Hkv, D, R)
+    want = pda.pda_norm_rotary(c.q, c.pos_arg, c.k, **c.kw_args)
+    rows = c.rows.clone()
+    q, k = rows[:, :Hq], rows[:, Hq:Hq + Hkv]
+    pda.pda_norm_rotary(q, c.pos_arg, k, q_out=q, k_out=k, **c.kw_args)
+    assert torch.equal(q[c.real], want[0][c.real]) and torch.equal(k[c.real], want[1][c.real])
+    assert torch.equal(rows[~c.real], c.rows[~c.real]) and torch.equal(rows[:, Hq + Hkv:], c.rows[:, Hq + Hkv:])
+
+
 def test_more_tokens_than_workgroups():
     """2^20 workgroups of 4 tokens, and some."""
     c = heads.Case(4 * 2 ** 20 + 77, 1, 0, 16, 16)

@@ -41,7 +41,9 @@ typedef struct pda_window {
 int pda_plan_window(const pda_problem *prob, const pda_window *window, pda_plan_info *plan);
 
 /* The attention of one step; out is fp32 [B][n][Hq][D], rows that see nothing are
- * zero.  Everything is computed to fp32 accuracy.  `workspace`: any contents, pda_plan_window()'s workspace_bytes, 16-byte
+ * zero.  Everything is computed to fp32 accuracy: with scores of the order of 1 (in units of log2) an
+ * output is off by less than 1e-6 of its norm; what larger scores add is fp32's rounding of them.
+ * `workspace`: any contents, pda_plan_window()'s workspace_bytes, 16-byte
  * aligned (NULL where that is 0); calls that overlap on the GPU need separate ones.  Results are bit-for-bit
  * reproducible for a descriptor. */
 int pda_decode_window(const pda_problem *prob, const pda_window *window, const void *q, const void *k_cache,

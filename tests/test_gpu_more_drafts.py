@@ -1,0 +1,103 @@
+"""Drafted tokens through the whole chain, against 64 bits: blocks for them, their keys and values stored, attention,
+the rejected ones put back, and the next drafts written where they were."""
+import numpy as np
+import pytest
+import torch
+
+import more_reference as ref
+import paper_2405_11143_amd as pda
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def i32(x):
+    return torch.tensor([int(y) for y in x], dtype=torch.int32, device="cuda")
+
+
+class Engine:
+    """A running batch: its cache and block tables on the GPU, and beside them the rows that the cache should hold."""
+
+    def __init__(self, B, NB, width, Hq, Hkv, D, window, sinks):
+        self.B, self.NB, self.width, self.Hq, self.Hkv, self.D, self.window, self.sinks = B, NB, width, Hq, Hkv, D, window, sinks
+        self.gen = torch.Generator().manual_seed(D)
+        self.pool, self.model = pda.new_block_pool(B, NB, width), ref.Pool(B, NB, width)
+        self.kc = torch.full((NB, Hkv, D // 8, 16, 8), float("nan"), dtype=BF, device="cuda")
+        self.vc = torch.full((NB, Hkv, 16, D), float("nan"), dtype=BF, device="cuda")
+        self.inv_freq = torch.from_numpy(10000.0 ** (-2.0 * np.arange(D // 2) / D)).cuda()
+        qw, self.kw = ((1 + 0.2 * torch.randn(D, generator=self.gen)).to(BF).cuda() for _ in range(2))
+        self.norm, self.rotary = pda.make_head_norm(qw, self.kw), pda.make_rotary(self.inv_freq)
+        self.K, self.V = (np.full((B, 16 * width, Hkv, D), np.nan) for _ in range(2))
+
+    def check_pool(self):
+        table, held, free, counts = (t.cpu().numpy() for t in self.pool.tensors)
+        np.testing.assert_array_equal(held, self.model.held)
+        np.testing.assert_array_equal(free[:counts[0]], self.model.free)
+        for b in range(self.B):
+            np.testing.assert_array_equal(table[b, :held[b]], self.model.table[b, :held[b]])
+        assert counts[1] == self.model.short
+
+    def resize(self, lens):
+        pda.pda_blocks_resize(self.pool, i32(lens))
+        self.model.resize(lens)
+        self.check_pool()
+
+    def store(self, lens, counts):
+        """Grown to lens, of which the last counts[b] tokens are new: their queries [T][Hq][D]."""
+        start = np.concatenate([[0], np.cumsum(counts)])
+        T = int(start[-1])
+        positions, slots = i32([9] * T), i32([9] * T)
+        pda.pda_blocks_resize(self.pool, i32(lens), i32(start), positions, slots)
+        self.model.resize(lens)
+        self.check_pool()
+        rows = torch.randn((T, self.Hq + 2 * self.Hkv, self.D), generator=self.gen).to(BF).cuda()
+        q, k, v = rows[:, :self.Hq], rows[:, self.Hq:self.Hq + self.Hkv], rows[:, self.Hq + self.Hkv:]
+        q_out = pda.pda_norm_rotary_append(q, k, v, positions, slots, self.kc, self.vc, self.norm, self.rotary)
+        axis = torch.zeros(self.D // 2, dtype=torch.uint8, device="cuda")
+        exact = ref.turned(ref.normed(k.double(), self.kw, 1e-6), positions[None], self.inv_freq, axis, False)[0].cpu().numpy()
+        stored_k = self.kc.transpose(2, 3).reshape(self.NB, self.Hkv, 16, self.D).double().cpu().numpy()
+        stored_v, v = self.vc.double().cpu().numpy(), v.double().cpu().numpy()
+        for b in range(self.B):
+            for i, t in enumerate(range(lens[b] - counts[b], lens[b])):
+                if t >= 16 * self.model.held[b]:
+                    continue  # (not granted)
+                at, r = (self.model.table[b, t // 16], slice(None), t % 16), start[b] + i
+                np.testing.assert_allclose(stored_k[at], exact[r], rtol=2.0 ** -8, atol=2.0 ** -17)
+                np.testing.assert_array_equal(stored_v[at], v[r])
+                self.K[b, t], self.V[b, t] = stored_k[at], stored_v[at]
+        return q_out
+
+    def attend(self, q, lens, on_device=None):
+        """q [B][n][Hq][D] over lens (or these lengths, on the GPU): checked, and returned."""
+        out = pda.pda_decode_window(q, self.kc, self.vc, self.pool.tensors[0], i32(lens) if on_device is None else on_device,
+                                    self.D ** -0.5, window=self.window, sinks=self.sinks, max_context_len=16 * self.width)
+        blocks = lambda x: x.reshape(self.B * self.width, 16, self.Hkv, self.D).swapaxes(1, 2)
+        table = np.arange(self.B * self.width).reshape(self.B, self.width)
+        want, unit = ref.window_attention(q.double().cpu().numpy(), blocks(self.K), blocks(self.V), table, lens, self.D ** -0.5,
+                                          self.window, self.sinks)
+        got = out.double().cpu().numpy()
+        assert (np.abs(got - want) <= unit * 2.0 ** -24).all()
+        return got
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (6, 1, 128)])
+@pytest.mark.parametrize("n", [5, 20])  # of 20, all rows of the wide kernel; 5 take one or two tiles
+def test_rejected_drafts_are_overwritten(Hq, Hkv, D, n):
+    e = Engine(3, 60, 12, Hq, Hkv, D, 40, 4)
+    lens = np.array([60, 3, 29])
+    e.store(lens, lens)
+    rng = np.random.RandomState(n)
+    crossed = 0
+    for step in range(6):
+        kept = rng.randint(0, n + 1, 3) if step else np.array([0, 0, 1])
+        q = e.store(lens + n, [n] * 3).view(3, n, Hq, D)
+        e.attend(q, lens + n)
+        crossed += int((-(-(lens + n) // 16) > -(-(lens + kept) // 16)).sum())
+        lens = lens + kept
+        e.resize(lens)  # the blocks of the rejected ones go back
+        one = e.store(lens + 1, [1] * 3).view(3, 1, Hq, D)  # and a token of the model's own
+        lens = lens + 1
+        e.attend(one, lens)
+    assert crossed >= 4
+    e.resize([0, 0, 0])
+    assert sorted(e.model.free) == list(range(60))

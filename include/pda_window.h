@@ -14,8 +14,10 @@
  * read: entries of blocks that lie behind every window and past the sinks may hold
  * anything, so a caller may give those blocks to other sequences.  Tokens that a row does
  * not see never reach its result, whatever their slots hold (NaN included; its rounding
- * may depend on the other rows of its work item); a NaN or infinite element of a token
- * makes the rows that see it non-finite.  A block id outside the pool among those read
+ * may depend on the other rows of its work item).  Of the tokens that it sees, one whose score is NaN
+ * or plus infinity makes the row non-finite, and a NaN or infinite element of a value the row's
+ * element there; one whose score is minus infinity counts nothing, and a row that sees no others is zero,
+ * as if it saw nothing.  A block id outside the pool among those read
  * makes the rows of the work item that meets it NaN.
  */
 #ifndef PDA_WINDOW_H

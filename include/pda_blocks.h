@@ -23,6 +23,9 @@
  *     becomes the number of blocks that are missing for all to be granted (0: all were).
  * So a length of 0 releases a sequence, growing and then shrinking to the old lengths
  * restores table, `held` and stack, and the outcome depends on the contents alone.
+ * Past its `held`, a row that was not granted may name blocks that it gave back and other rows own by
+ * now: given that row's length, attention would read their tokens.  A caller whose blocks may run short
+ * gives attention a length of 0 where 16 held[b] < L, formed from `held` on the GPU: the row is left out.
  *
  * Slot maps.  Row r of a packed batch of new tokens, row_start[b] <= r <
  * row_start[b + 1], is new token i = r - row_start[b] of sequence b, whose last new

@@ -1488,7 +1488,9 @@ def bind_blocks_resize(pool: pda_block_pool, context_lens, row_start=None, posit
     and/or slots (int32 [num_rows]) the slot map of the new tokens is written to them: row_start int32
     [num_seqs + 1] says whose they are, None: the same number of every sequence.  `workspace`: uint8 zeros
     of pda_blocks_workspace_bytes, allocated here when not given.  Calling it returns
-    (block_table, positions, slots)."""
+    (block_table, positions, slots).  Where blocks may run short, attention takes the lengths
+    torch.where(16 * held < context_lens, 0, context_lens): a row that was not granted its blocks names
+    others' in the entries that it does not hold."""
     import torch
 
     _check_lens(context_lens, pool.num_seqs)

@@ -1,5 +1,6 @@
 """Drafted tokens through the whole chain, against 64 bits: blocks for them, their keys and values stored, attention,
-the rejected ones put back, and the next drafts written where they were."""
+the rejected ones put back, and the next drafts written where they were; and batches whose blocks
+are short."""
 import numpy as np
 import pytest
 import torch
@@ -101,3 +102,30 @@ def test_rejected_drafts_are_overwritten(Hq, Hkv, D, n):
     assert crossed >= 4
     e.resize([0, 0, 0])
     assert sorted(e.model.free) == list(range(60))
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_a_sequence_without_its_blocks_is_left_out(n):
+    """Its row still holds the ids of blocks that it gave back and others own by now: a length of 0 where the row holds less
+    than its length, formed on the GPU, keeps attention off them."""
+    Hq, Hkv, D = 8, 2, 64
+    e = Engine(3, 14, 12, Hq, Hkv, D, 40, 4)
+    lens = np.array([60, 33, 60])
+    e.store(lens, lens)  # 4 + 3 + 4 blocks of 14
+    e.resize([60, 33, 17])
+    e.store([60, 62, 17], [0, 29, 0])  # the second takes what the third gave back
+    asked = np.array([60 + n, 62 + n, 128])
+    q = e.store(asked, [n, n, 111])  # 6 more for the third: not there
+    assert e.model.short > 0
+    table, held = (t.cpu().numpy() for t in e.pool.tensors[:2])
+    assert set(table[2, held[2]:4]) & set(table[1, :held[1]])
+    granted = torch.where(16 * e.pool.tensors[1] < i32(asked), 0, i32(asked))
+    assert granted.tolist() == [60 + n, 62 + n, 0]
+    got = e.attend(torch.stack([q[:n], q[n:2 * n], q[-n:]]), granted.tolist(), granted)
+    assert (got[2] == 0).all() and (got[:2] != 0).any(-1).all()
+    # the first is released: what the third asked for is there
+    asked[0] = 0
+    q = e.store(asked, [0, n, 111])
+    assert e.model.short == 0
+    got = e.attend(torch.stack([torch.zeros_like(q[:n]), q[:n], q[-n:]]), asked)
+    assert (got[0] == 0).all() and (got[1:] != 0).any(-1).all()

@@ -76,12 +76,14 @@ int pda_blocks_workspace_bytes(const pda_block_pool *pool, size_t *bytes);
  * NULL), write the slot map of its rows.  `workspace`: pda_blocks_workspace_bytes() bytes,
  * 16-byte aligned, filled with ZEROS before its first use; a call leaves it ready for the
  * next one (of any pool), and calls that overlap on the GPU need separate ones.
- * context_lens, row_start, positions and slots overlap no buffer of the pool. */
+ * context_lens, row_start, positions and slots overlap no buffer of the pool; positions and slots
+ * overlap no other buffer of the call at all (PDA_ERR_VALUE). */
 int pda_blocks_resize(const pda_block_pool *pool, const int32_t *context_lens, const pda_token_rows *rows,
                       void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* The slot map alone, for a block table however it was made (every entry counts as
- * held).  positions and slots may not both be NULL unless num_rows is 0. */
+ * held).  positions and slots may not both be NULL unless num_rows is 0, and overlap no other
+ * buffer of the call (PDA_ERR_VALUE). */
 int pda_slot_map(int32_t num_seqs, int32_t num_blocks, int32_t max_blocks_per_seq, const int32_t *block_table,
                  const int32_t *context_lens, const pda_token_rows *rows, hipStream_t stream);
 

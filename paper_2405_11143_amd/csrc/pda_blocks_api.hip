@@ -36,6 +36,24 @@ size_t workspace_of(int32_t num_seqs) {
   return num_seqs == 0 ? 0 : 4 * sizeof(int32_t) + (size_t)num_seqs * sizeof(pda::BlockMove);
 }
 
+bool overlap(const void* p, size_t bytes, const void* q, size_t more) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && bytes > 0 && more > 0 && (a < b ? b - a < bytes : a - b < more);
+}
+
+// Workgroups read lengths, row starts and ids while others write the map.
+int check_apart(const pda::BlocksArgs& a, size_t workspace_bytes) {
+  const size_t n = 4 * (size_t)a.rows.num_rows, seqs = 4 * (size_t)a.pool.num_seqs;
+  for (const int32_t* out : {a.rows.positions, a.rows.slots}) {
+    if (overlap(out, n, a.lens, seqs) || overlap(out, n, a.rows.row_start, seqs + 4) ||
+        overlap(out, n, a.table, seqs * (size_t)a.pool.max_blocks_per_seq) || overlap(out, n, a.pool.held, seqs) ||
+        overlap(out, n, a.pool.free_blocks, 4 * (size_t)a.pool.num_blocks) || overlap(out, n, a.pool.counts, 8) ||
+        overlap(out, n, a.arrived, workspace_bytes))
+      return PDA_ERR_VALUE;
+  }
+  return overlap(a.rows.positions, n, a.rows.slots, n) ? PDA_ERR_VALUE : PDA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -72,6 +90,8 @@ int pda_blocks_resize(const pda_block_pool* pool, const int32_t* context_lens, c
   a.arrived = static_cast<int32_t*>(workspace);
   a.totals = a.arrived + 2;
   a.moves = reinterpret_cast<pda::BlockMove*>(a.totals + 2);
+  rc = check_apart(a, workspace_of(pool->num_seqs));
+  if (rc != PDA_OK) return rc;
   const hipError_t e = pool->num_seqs > 0 ? pda::launch_blocks_resize(a, stream) : pda::launch_slot_map(a, stream);
   return e == hipSuccess ? PDA_OK : PDA_ERR_HIP;
 }
@@ -93,6 +113,8 @@ int pda_slot_map(int32_t num_seqs, int32_t num_blocks, int32_t max_blocks_per_se
   a.table = block_table;
   a.moves = nullptr;
   a.totals = a.arrived = nullptr;
+  rc = check_apart(a, 0);
+  if (rc != PDA_OK) return rc;
   return pda::launch_slot_map(a, stream) == hipSuccess ? PDA_OK : PDA_ERR_HIP;
 }
 

@@ -7,7 +7,8 @@
  * heads, one for all key heads), becomes
  *   u = x / sqrt(mean_d x_d^2 + eps),  z = u * (w + weight_offset),  y = R z
  * where R turns the first rotary_dim elements in pairs as pda_rotary says
- * (pda_fp8.h).  Everything is computed in fp32 (angles in 64 bits) and rounded once.
+ * (pda_fp8.h).  Everything is computed in fp32 and rounded once; an angle is formed in 64 bits, whole
+ * turns are taken off it, and what is left is fp32, within 2^-25 turns however far the position.
  * Either step may be left out: `norm` NULL, `rotary` NULL.
  *
  * Several axes.  With pda_rotary_axes a token has a position on each axis (time,
@@ -20,8 +21,8 @@
  * contiguous: the parts of a fused projection's rows can be used where they lie.
  * num_kv_heads 0: no keys.  dtype PDA_DTYPE_BF16 or PDA_DTYPE_F32, the same for all rows of a
  * call.  D is a multiple of 8, at most 512; pointers and rows are 16-byte aligned.
- * Elements are below 2^59 in magnitude (their squares are summed in fp32); with eps 0 a
- * row's largest is above 2^-59.
+ * Elements are below 2^59 in magnitude (their squares are summed in fp32); with eps below 2^-118 a
+ * row's largest is above 2^-59, or all are zero.
  * `positions` is device int32 [T], or [num_axes] rows of T.  A token whose position
  * (on the first axis) is negative is padding: its rows are neither read nor
  * written.  Positions on further axes may have either sign.

@@ -13,7 +13,7 @@ constexpr int kWgChunks = 2 * kWaves;  // chunks of a workgroup
 constexpr int kStageBlocks = 2;        // blocks of a staged step: 32 tokens
 constexpr int kBuffers = 4;            // one step folded, the next one's scores formed, two in flight
 constexpr int kWindow = 1024;          // block ids held in LDS at a time
-constexpr float kExactMax = 128.f;     // running maxima whose rounding is below P's resolution
+constexpr float kExactMax = 128.f;     // running maxima that may be rounded: by up to 2^-18, as a score of their size is
 
 template <int D>
 struct WideLds {

@@ -21,3 +21,22 @@ def test_accuracy(D, Hq, Hkv, n, partition_tokens):
     rel = float(np.sqrt(((got - want) ** 2).sum() / (want ** 2).sum()))
     print(f"D={D} {Hq}/{Hkv} n={n} Tp={partition_tokens}: {rel:.2e} of the norm", flush=True)
     assert rel <= acc.BAR
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 8, 40])
+@pytest.mark.parametrize("partition_tokens", [0, 96])
+@pytest.mark.parametrize("size", [8, 24])
+def test_larger_scores_add_their_rounding_alone(D, n, partition_tokens, size):
+    """Scores `size` times as large, up to about 30 and 90: plain fp32 operations round each once where it is scaled, by up to
+    2^-18 at 64 to 128.  The kernels may round a row's maximum by as much beside it, from one step to
+    another: no more than twice the error."""
+    q, k, v, table, lens = acc.inputs(8, 2, D, n, 30 + n)
+    scale = size * D ** -0.5
+    in_bits = lambda kind: [x.float().numpy().astype(kind) for x in (q, k, v)]
+    want, _ = window_attention(*in_bits(np.float64), table, lens, scale, acc.WINDOW, acc.SINKS)
+    plain, _ = window_attention(*in_bits(np.float32), table, lens, scale, acc.WINDOW, acc.SINKS)
+    got = windows.run(q, k, v, table, lens, acc.WINDOW, acc.SINKS, scale, partition_tokens=partition_tokens).cpu().double().numpy()
+    off = lambda x: float(np.sqrt(((x - want) ** 2).sum() / (want ** 2).sum()))
+    print(f"D={D} n={n} Tp={partition_tokens} x{size}: {off(got):.2e} of the norm, plain {off(plain):.2e}", flush=True)
+    assert off(got) <= 2 * off(plain) + acc.BAR

@@ -58,6 +58,8 @@ typedef struct pda_rotary_axes {
 
 /* y of q into q_out and of k into k_out.  An output may be its own input (same
  * pointer and stride); otherwise it overlaps no other buffer of the call.  `axes` NULL: one.
+ * (The rotation alone on one axis is pda_rotary_apply, the faster call for it; the two agree but for the last
+ * rounding.)
  * Without `norm`, rotary->backward 1 turns back (the gradient of the rotation);
  * with it, backward must be 0.  `norm` and `rotary` may not both be NULL. */
 int pda_norm_rotary(const pda_head_norm *norm, const pda_rotary *rotary, const pda_rotary_axes *axes,

@@ -13,7 +13,11 @@
 // a thread to a sequence, and takes its share of the ids and of the slot map; the last one to
 // have read the held counts writes the new ones.  For more, one workgroup forms the sums and
 // the new counts (plan_kernel); then a workgroup for every kSpan entries of every row moves
-// that row's ids and writes the slots of the tokens in those blocks (move_kernel).
+// that row's ids and writes the slots of the tokens in those blocks (move_kernel).  5 new tokens of
+// every sequence and back, two calls: 1024 sequences 13.6 us, 1025 24, 4096 49, 16384 169, most of it in the one workgroup.
+// A slot map alone is move_kernel's second half, whose grid follows the table's width: a decode step's of 256
+// sequences 3.9 us over tables of 4096 entries, 30 over tables of 65536, of whose 65792 workgroups 256 have work;
+// of 48 prompts, 92000 rows, 5.1.
 #include <algorithm>
 
 #include "pda_blocks_internal.h"

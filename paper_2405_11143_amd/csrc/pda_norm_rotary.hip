@@ -13,6 +13,15 @@
 // values into the cache 96 us, 5.0 TB/s; 6000 tokens of 28 + 4 heads, three axes, rotation alone, 22.3 us
 // (17.8 with rows that the last-level cache holds); 4097 of 16 + 16 heads of 64 in fp32, two axes,
 // turned back, 18.8 us (16.1); 256 tokens of a decode step into the cache 5.1 us, of which the launch is 4.4.
+// The gradient in fp32, 16384 of 32 + 8, 199 us, 5.1 TB/s; of 16 + 16 heads of 80 116 us (floor 99), in bf16 80 (49),
+// the forward 44 (33): 5 of a row's 8 lanes have elements.
+//
+// Tokens of few heads are furthest from the bytes: a step's rows are of one kind and one token, so 8 + 2 heads
+// of 64 fill 10 of 32 places, with values 12 of 48.  60000 tokens of them 53 us (floor 30), 54000 into the cache 77 (32);
+// of 4 + 1 heads of 128 51 and 76.
+//
+// The rotation alone on one axis is what rotary_kernel (pda_rotary.hip) does, and that is the faster there:
+// 16384 tokens of 32 + 8 heads 61 us here and 60 there, 6000 of 28 + 4 17.5 and 16.7, 60000 of 8 + 2 of 64 49 and 36.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,8 +39,12 @@ constexpr int kComputeUnits = 256;
 constexpr int kFewWaves = 4096;  // wavefronts that fewer tokens are split into
 // From so many tokens on, rows of whole cache lines go out with the non-temporal hint.  32 + 8 heads of 128,
 // us, without / with: 256 tokens 5.0 / 5.0, 512 5.4 / 4.9, 1024 7.2 / 6.2, 1500 9.1 / 7.6, 2500 13.8 / 10.6, 16384 65.2
-// / 59.2; into the cache 26000 of 28 + 4 101.7 / 96.0.  With a kernel behind it that reads the queries the
-// two take 9.2 / 8.9 for 512, 12.9 / 11.7 for 1024, 20.2 / 21.7 for 3000.
+// / 59.2; into the cache 26000 of 28 + 4 101.7 / 96.0.  The line is that of the call alone: a kernel behind it that
+// reads the rows finds fewer of them in the caches, and from about 2000 tokens on loses what the hint gains, or more.
+// With one that reads the queries, the two take 9.0 / 8.9 for 512, 13.0 / 11.7 for 1024, 18.2 / 18.4 for 2048,
+// 20.5 / 22.0 for 3000, 53.2 / 55.4 for 8192, 107 / 110 for 16384; the append with attention over a window of 64
+// behind it 25.7 / 25.2 for 1024, 45.0 / 47.3 for 3000, 104 / 109 for 8192, 208 / 212 for 16384; the gradient with a
+// product over its rows 27.0 / 26.8 for 1024, 47.6 / 50.5 for 3000, 98 / 104 for 8192, 199 / 205 for 16384.
 constexpr int kHintTokens = 512;
 
 // 8 elements as they lie in memory.

@@ -11,7 +11,9 @@
 //
 // Measured: 256 sequences of 32 / 8 heads of 128 past a window of 1024 167 us, 6.3 TB/s, 94% of
 // what a bare gather of such tiles reaches; four wavefronts to a SIMD, whose registers hold one
-// tile less in flight, 184; 5 new tokens of each 190; 8 long samples, a window of 4096, 19.4 with the merge.
+// tile less in flight, 184; 5 new tokens of each 190; 8 long samples, a window of 4096, 19.4 with the merge, whose launch
+// is 3.4 of them.  For two tiles at D = 128 set_apart, inlined though it hardly ever runs, makes the kernel spill (36
+// bytes of scratch a lane).
 #include "pda_wave.h"
 #include "pda_window_internal.h"
 

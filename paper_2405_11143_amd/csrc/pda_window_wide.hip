@@ -11,11 +11,16 @@
 //
 // Bound by the matrix pipes (49% busy, at 1.9 GHz) and vector issue (50%) beside each other: with P in three
 // bf16 parts a step is 4 products where the mathematics has 2.  512 new tokens of 32 sequences (32 / 8
-// heads of 128) over a window of 1024: 551 us, 500 TFLOP/s by what the rows see, 1030 by what is
-// issued, 85% of what a large library product reaches; over whole contexts of 4096, where few steps are masked
-// and a workgroup takes 128, 570 and 1140, 94%.  A barrier for every second step only: 1% less time.  With P in two parts, rounded to nearest, 485 us and
+// heads of 128) over a window of 1024: 551 to 568 us on different cards, 480 to 500 TFLOP/s by what the rows
+// see, 1000 to 1030 by what is issued, 82 to 85% of what a large library product reaches; over whole contexts of
+// 4096, where few steps are masked and a workgroup takes 128, 570 and 1140, 94%.  A barrier for every second step only: 1% less time.  With P in two parts, rounded to nearest, 485 us and
 // results 2.4e-6 of their norm off instead of 4.5e-7 (plain fp32 operations: 7e-7); three parts rounded to
 // nearest 570.  Before, with two parts: steps of 32 aligned tokens 10% more, rows stored through LDS 2%.
+//
+// A wavefront has up to 32 rows, so with 33 to 64 per KV head two of the four have none: they load, and the
+// products run on half of the SIMDs.  256 contexts of 512 to 4096, a window of 1024, the same heads, against a
+// gather of the tokens that are seen: 9 new ones (36 rows) 245 / 165 us, 16 (64) 259 / 173, 31 (124) 331 / 189,
+// 64 (two workgroups) 596 / 224; 5 (20, pda_window.hip) 189 / 161.
 #include "pda_wide.h"
 #include "pda_window_internal.h"
 
